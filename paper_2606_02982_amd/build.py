@@ -17,7 +17,9 @@ ARCH = "gfx950"
 
 SOURCES = ["api.hip", "characterize.hip", "sort.hip", "calibrate.hip", "score.hip", "order.hip", "stats.hip",
            "sim.hip", "ssort.hip", "calchunk.hip", "agmerge.hip",
-           "lsort.hip", "norder.hip"]
+           "lsort.hip", "norder.hip",
+           "serve.hip", "decode.hip", "attend_bf16.hip", "attend_f16.hip", "attend_bf16_e4m3.hip",
+           "attend_f16_e4m3.hip", "evict.hip", "verify.hip"]
 
 HIP_FLAGS = [
     "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -9,6 +9,7 @@
 #include <mutex>
 
 #include "../../include/driftsched.h"
+#include "apiutil.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -22,44 +23,6 @@ static_assert(DS_WRR_BLOCKED == ds::kWrrBlocked && DS_WRR_SMOOTH == ds::kWrrSmoo
 using namespace ds;
 
 namespace {
-
-constexpr size_t kFlagBytes = 256;   // validation word at the start of every workspace
-
-ds_status hip_status(hipError_t e) { return e == hipSuccess ? DS_OK : DS_ERR_HIP; }
-
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// Runs the enqueue function twice under DS_VALIDATE: first the data checks
-// (with a cleared flag), then, if the stream reports no violation, the work.
-template <typename F>
-ds_status run(void *ws, uint32_t flags, hipStream_t s, F &&enqueue)
-{
-    uint32_t *flag = static_cast<uint32_t *>(ws);
-    if (flags & DS_VALIDATE) {
-        hipError_t e = fill_u32(flag, 0u, 1, s);
-        if (e == hipSuccess) e = enqueue(flag);
-        uint32_t host = 0;
-        if (e == hipSuccess) e = hipMemcpyAsync(&host, flag, 4, hipMemcpyDeviceToHost, s);
-        if (e == hipSuccess) e = hipStreamSynchronize(s);
-        if (e != hipSuccess) return DS_ERR_HIP;
-        if (host) return DS_ERR_DATA;
-    }
-    return hip_status(enqueue(nullptr));
-}
-
-void *after_flag(void *ws) { return static_cast<uint8_t *>(ws) + kFlagBytes; }
-
-// The integer a C caller passed for an enum-typed argument. C allows any int
-// there; in C++ a value outside the enumeration's range may not be read as
-// the enum type, so it is copied out as bytes first.
-template <typename E>
-int enum_int(const E &e)
-{
-    static_assert(sizeof(E) == sizeof(int), "the ABI's enums are int-sized");
-    int v;
-    memcpy(&v, &e, sizeof v);
-    return v;
-}
 
 // The calls whose kernels wait on each other (the look-backs of the sorts)
 // keep a status word in the workspace, at byte DS_WS_STATUS_OFFSET: the
@@ -124,12 +87,6 @@ size_t ds_workspace_bytes(ds_op op_arg, uint64_t n, uint32_t n_groups)
         return n_groups >= 1 && n_groups <= DS_SIM_MAX_RUNS ? kFlagBytes + sim_ws_bytes(n, n_groups) : 0;
     }
     return 0;
-}
-
-static ds_status check_ws(void *ws, size_t ws_bytes, size_t need)
-{
-    if (!ws || ws_bytes < need || !aligned(ws, 256)) return DS_ERR_WORKSPACE;
-    return DS_OK;
 }
 
 ds_status ds_characterize(const uint8_t *text, uint64_t text_bytes, const uint64_t *offsets,

@@ -1,0 +1,469 @@
+// Attention of the newest tokens over a paged cache: the kernel (included by
+// one source per element type, attend_*.hip).
+//
+// With q scaled by scale * log2(e), every query keeps the running maximum m
+// of its scores s_j, the sum l = sum_j 2^(s_j - m) and o = sum_j 2^(s_j - m)
+// v_j, and rescales l and o when m grows; out = o / l. Splits of the cache
+// and the four waves of a workgroup hold (m, l, o) of their own tokens and
+// are joined by the same rule.
+//
+// The work is reading the cache once: 4 dim bytes per token and head in 16
+// bits against 4 dim flops per query row. So the loop is laid out for loads:
+// a wave takes 32 tokens at a time straight from memory into the operand
+// layout of the matrix instructions, with no pass through shared memory.
+//  - scores: S^T = K Q^T in 16x16x32 steps. Lane (m, g) of K holds token m,
+//    dimensions 8 g .. of each 32 (16 g .. of each 64 in 8 bits: the order of
+//    a sum's terms is free, so a load is always 16 bytes).
+//  - S^T leaves the tokens 4 g + i of column m (a query) in lane (m, g); this
+//    is taken as the order of the 32 tokens in the second product, so the
+//    weights are its operand where they stand.
+//  - O^T = V^T P^T: lane (m, g) loads dimensions 8 m .. 8 m + 7 of its eight
+//    tokens, a row of V by 16 lanes, and swaps 16-bit halves between its own
+//    registers to get one dimension of eight tokens.
+// Weights are split into two 16-bit parts (value and remainder), so that
+// rounding them adds nothing to out's own rounding; the matrix units are idle
+// most of the time anyway.
+#pragma once
+
+#include "common.h"
+#include "serve.h"
+
+namespace ds {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+
+struct Bf16 {
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ floatx4 mfma(uintx4 a, uintx4 b, floatx4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        const floatx2 v = {a, b};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, x2));
+    }
+    static __device__ __forceinline__ float lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+    static __device__ __forceinline__ float hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+    // two 8-bit floats, exact
+    template <bool kHigh>
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t w)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, kHigh));
+    }
+};
+
+struct F16 {
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ floatx4 mfma(uintx4 a, uintx4 b, floatx4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        const floatx2 v = {a, b};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, x2));
+    }
+    static __device__ __forceinline__ float lo(uint32_t w) { return (float)__builtin_bit_cast(x2, w)[0]; }
+    static __device__ __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(x2, w)[1]; }
+    template <bool kHigh>
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t w)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, kHigh));
+    }
+};
+
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.0f : m; }
+
+// One workgroup: the tokens of one split for one unit (see DecodeArgs).
+// kDim: padded dimensions; kTiles: 16-row tiles; kPage16: pages hold a
+// multiple of 16 tokens, so that half a block lies in one page and its
+// address is the same for the whole wave.
+template <typename T, bool kE4m3, int kDim, int kTiles, bool kPage16>
+__global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
+{
+    constexpr int kStepsK = kDim / 32;                  // matrix steps per score
+    constexpr int kLoadsK = kE4m3 ? kDim / 64 : kDim / 32;
+    constexpr int kParts = kDim > 128 ? kDim / 128 : 1; // V: pieces of a row
+    constexpr int kVd = kDim / 16 / kParts;             // V: dimensions per lane and piece
+    constexpr int kOut = kDim / 16;                     // 16-dimension tiles of O^T
+    constexpr int kElem = kE4m3 ? 1 : 2;
+    constexpr int kRows = 16 * kTiles;
+    constexpr int kPitch = kDim + 4;
+
+    __shared__ float sm_m[4][kRows], sm_l[4][kRows];
+    __shared__ __align__(16) float sm_o[kRows * kPitch];
+
+    const KvView &c = a.c;
+    const int lane = lane_id(), m = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const uint32_t split = blockIdx.x % a.n_splits;
+    const uint32_t unit = blockIdx.x / a.n_splits;
+    const uint32_t tile = unit % a.n_tiles;
+    const uint32_t head = unit / a.n_tiles % c.n_kv;
+    const uint32_t row = unit / a.n_tiles / c.n_kv;
+    const uint32_t req = a.rows ? a.rows[row] : row;
+    const uint32_t n_all = req < c.n_requests ? c.len[req] : 0;
+    const uint32_t n = n_all < c.cap ? n_all : c.cap;
+    const Span span = span_of(n, a.tokens, a.window, a.sinks);
+    const uint32_t v0 = split * a.split_blocks;
+    if (split > 0 && v0 >= span.total) return;
+    const uint32_t v1 = v0 + a.split_blocks < span.total ? v0 + a.split_blocks : span.total;
+
+    const uint32_t query_rows = a.group * a.tokens;
+    const int first_pos = (int)n - (int)a.tokens;       // of the first query
+    const int lo = a.window && first_pos >= (int)a.window ? first_pos - (int)a.window + 1 : 0;
+
+    // this lane's queries (one column of each tile)
+    uintx4 q[kTiles][kStepsK];
+    int pos[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; t++) {
+        const uint32_t r = tile * kRows + t * 16 + m;
+        const uint32_t tok = r / a.group, h = r % a.group;
+        pos[t] = r < query_rows ? first_pos + (int)tok : -1;
+        const uint16_t *src = static_cast<const uint16_t *>(a.q) + row * a.q_row + tok * a.q_token +
+                              ((uint64_t)head * a.group + h) * a.q_head;
+#pragma unroll
+        for (int s = 0; s < kStepsK; s++) {
+            const uint32_t d = kE4m3 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+            q[t][s] = uintx4{0, 0, 0, 0};
+            if (r < query_rows && d < c.dim) q[t][s] = *reinterpret_cast<const uintx4 *>(src + d);
+        }
+    }
+    const float scale = a.scale2 * (kE4m3 && c.k_scale ? c.k_scale[head] : 1.0f);
+    const uint32_t *table = c.table + (uint64_t)req * c.max_pages;
+    const uint8_t *kh = c.k + head * c.head_stride * kElem;
+    const uint8_t *vh = c.v + head * c.head_stride * kElem;
+    float *scores = a.scores;
+
+    auto block_of = [&](uint32_t v) { return v < span.sink_blocks ? v : span.first_block + (v - span.sink_blocks); };
+    // pages of the two halves of block v (kPage16)
+    auto pages_of = [&](uint32_t v, uint32_t *page) {
+        const uint32_t j0 = block_of(v) * kBlockTokens;
+#pragma unroll
+        for (int i = 0; i < 2; i++) page[i] = j0 + 16 * i < n ? table[(j0 + 16 * i) / c.page_size] : 0xFFFFFFFFu;
+    };
+
+    float mx[kTiles], sum[kTiles];
+    floatx4 acc[kTiles][kOut];
+    // A pass in which 0 * inf or 0 * NaN of a token that some queries do not
+    // see reached the sums is taken again (careful), with every product made
+    // only where the token is seen.
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int t = 0; t < kTiles; t++) {
+            mx[t] = -__builtin_inff();
+            sum[t] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kOut; x++) acc[t][x] = floatx4{0, 0, 0, 0};
+        }
+        uint32_t page[2] = {0, 0};
+        if (kPage16 && v0 + wave < v1) pages_of(v0 + wave, page);
+        for (uint32_t v = v0 + wave; v < v1; v += 4) {
+            const int j0 = (int)(block_of(v) * kBlockTokens);
+            uint32_t seen = 0xFFFFFFFFu;                // tokens of the block that exist, by bit
+            uint64_t k_at[2], v_at[8];                  // element offsets of this lane's tokens
+            if (kPage16) {
+                uint64_t base[2];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const bool ok = page[i] < c.n_pages;
+                    if (!ok) seen &= i ? 0x0000FFFFu : 0xFFFF0000u;
+                    const uint32_t slot = (uint32_t)(j0 + 16 * i) % c.page_size;
+                    base[i] = (ok ? page[i] : 0u) * c.page_stride + slot * c.token_stride;
+                    k_at[i] = base[i] + m * c.token_stride;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; j++) v_at[j] = base[j >> 2] + (g * 4 + (j & 3)) * c.token_stride;
+            } else {
+                const uint32_t j = (uint32_t)j0 + (lane & 31);
+                const uint32_t pg = j < n ? table[j / c.page_size] : 0xFFFFFFFFu;
+                const bool ok = pg < c.n_pages;
+                seen = (uint32_t)__ballot(ok);
+                const uint64_t at = (ok ? pg : 0u) * c.page_stride + (j % c.page_size) * c.token_stride;
+                const int lo32 = (int)(uint32_t)at, hi32 = (int)(uint32_t)(at >> 32);
+                auto of = [&](int src) {
+                    return ((uint64_t)(uint32_t)__shfl(hi32, src, 64) << 32) | (uint32_t)__shfl(lo32, src, 64);
+                };
+#pragma unroll
+                for (int i = 0; i < 2; i++) k_at[i] = of(16 * i + m);
+#pragma unroll
+                for (int i = 0; i < 8; i++) v_at[i] = of((i >> 2) * 16 + g * 4 + (i & 3));
+            }
+            uintx4 kr[2][kLoadsK];
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int s = 0; s < kLoadsK; s++) {
+                    const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
+                    kr[i][s] = uintx4{0, 0, 0, 0};
+                    if (d < c.dim) kr[i][s] = *reinterpret_cast<const uintx4 *>(kh + (k_at[i] + d) * kElem);
+                }
+            // dimensions kVd m .. of part p, for the lane's eight tokens, as
+            // they are stored
+            constexpr int kVw = kVd * kElem / 4;        // 32-bit words per lane, token and part
+            uint32_t vr[8][kParts][kVw];
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+#pragma unroll
+                for (int p = 0; p < kParts; p++) {
+                    const uint32_t d = p * 128 + m * kVd;
+#pragma unroll
+                    for (int w = 0; w < kVw; w++) vr[j][p][w] = 0;
+                    if (d < c.dim) {
+                        const uint8_t *src = vh + (v_at[j] + d) * kElem;
+                        if constexpr (kVw == 4) {
+                            const uintx4 x = *reinterpret_cast<const uintx4 *>(src);
+#pragma unroll
+                            for (int w = 0; w < 4; w++) vr[j][p][w] = x[w];
+                        } else if constexpr (kVw == 2) {
+                            const uintx2 x = *reinterpret_cast<const uintx2 *>(src);
+                            vr[j][p][0] = x[0];
+                            vr[j][p][1] = x[1];
+                        } else {
+                            vr[j][p][0] = *reinterpret_cast<const uint32_t *>(src);
+                        }
+                    }
+                }
+            if (kPage16 && v + 4 < v1) pages_of(v + 4, page);
+
+            // which tokens any query sees; whether every query sees all
+            if ((int)n - j0 < 32) seen &= (1u << ((int)n - j0)) - 1u;
+            const bool full = seen == 0xFFFFFFFFu && j0 + 31 <= first_pos &&
+                              (a.window == 0 || j0 > (int)n - 1 - (int)a.window || j0 + 31 < (int)a.sinks);
+            if (!full) {
+                uint32_t near = 0xFFFFFFFFu;            // at or behind the window's start
+                if (lo > j0) near = lo - j0 < 32 ? ~((1u << (lo - j0)) - 1u) : 0u;
+                uint32_t sink = 0;
+                if ((int)a.sinks > j0) sink = (int)a.sinks - j0 < 32 ? (1u << ((int)a.sinks - j0)) - 1u : 0xFFFFFFFFu;
+                seen &= near | sink;
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const bool on = (seen >> ((j >> 2) * 16 + g * 4 + (j & 3))) & 1u;
+#pragma unroll
+                    for (int p = 0; p < kParts; p++)
+#pragma unroll
+                        for (int w = 0; w < kVw; w++) vr[j][p][w] = on ? vr[j][p][w] : 0u;
+                }
+            }
+
+            floatx4 s[kTiles][2];
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int t = 0; t < kTiles; t++) {
+                    s[t][i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+                    for (int st = 0; st < kStepsK; st++) {
+                        uintx4 kf;
+                        if constexpr (kE4m3) {
+                            const uint32_t w0 = kr[i][st >> 1][(st & 1) * 2], w1 = kr[i][st >> 1][(st & 1) * 2 + 1];
+                            kf = uintx4{T::template from_e4m3<false>(w0), T::template from_e4m3<true>(w0),
+                                        T::template from_e4m3<false>(w1), T::template from_e4m3<true>(w1)};
+                        } else {
+                            kf = kr[i][st];
+                        }
+                        s[t][i] = T::mfma(kf, q[t][st], s[t][i]);
+                    }
+                }
+            // softmax step: s becomes the weights
+            uintx4 p_hi[kTiles], p_lo[kTiles];
+#pragma unroll
+            for (int t = 0; t < kTiles; t++) {
+                float top = -__builtin_inff();
+#pragma unroll
+                for (int i = 0; i < 2; i++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        float x = s[t][i][e] * scale;
+                        if (!full) {
+                            const int bit = 16 * i + g * 4 + e, j = j0 + bit;
+                            const bool on = ((seen >> bit) & 1u) && j <= pos[t] &&
+                                            (a.window == 0 || j > pos[t] - (int)a.window || j < (int)a.sinks);
+                            x = on ? x : -__builtin_inff();
+                        }
+                        s[t][i][e] = x;
+                        top = fmaxf(top, x);
+                    }
+                if (scores) {
+                    const uint32_t r = tile * kRows + t * 16 + m;
+                    if (r < query_rows) {
+                        float *to = scores + (((uint64_t)row * c.n_kv + head) * query_rows + r) * a.score_len +
+                                    (uint64_t)v * kBlockTokens + g * 4;
+#pragma unroll
+                        for (int i = 0; i < 2; i++) *reinterpret_cast<floatx4 *>(to + 16 * i) = s[t][i];
+                    }
+                }
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                if (__any(top > mx[t])) {
+                    const float grown = fmaxf(mx[t], top);
+                    const float f = __builtin_amdgcn_exp2f(mx[t] - finite_or_zero(grown));
+                    mx[t] = grown;
+                    sum[t] *= f;
+#pragma unroll
+                    for (int x = 0; x < kOut; x++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) acc[t][x][e] *= f;
+                }
+                const float base = finite_or_zero(mx[t]);
+#pragma unroll
+                for (int i = 0; i < 2; i++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        s[t][i][e] = __builtin_amdgcn_exp2f(s[t][i][e] - base);
+                        sum[t] += s[t][i][e];
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; i++)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const uint32_t w = T::pack(s[t][i][e], s[t][i][e + 1]);
+                        p_hi[t][i * 2 + e / 2] = w;
+                        p_lo[t][i * 2 + e / 2] = T::pack(s[t][i][e] - T::lo(w), s[t][i][e + 1] - T::hi(w));
+                    }
+            }
+#pragma unroll
+            for (int p = 0; p < kParts; p++)
+#pragma unroll
+                for (int d = 0; d < kVd; d += 2) {
+                    uint32_t pair[8];                   // dimensions d, d + 1 of the eight tokens
+#pragma unroll
+                    for (int j = 0; j < 8; j++) {
+                        if constexpr (kE4m3)
+                            pair[j] = (d & 2) ? T::template from_e4m3<true>(vr[j][p][d >> 2])
+                                              : T::template from_e4m3<false>(vr[j][p][d >> 2]);
+                        else
+                            pair[j] = vr[j][p][d >> 1];
+                    }
+#pragma unroll
+                    for (int o = 0; o < 2; o++) {
+                        const int x = p * kVd + d + o;
+                        const uint32_t sel = o ? 0x07060302u : 0x05040100u;
+                        uintx4 vf;
+#pragma unroll
+                        for (int w = 0; w < 4; w++) vf[w] = __builtin_amdgcn_perm(pair[2 * w + 1], pair[2 * w], sel);
+                        if (!careful) {
+#pragma unroll
+                            for (int t = 0; t < kTiles; t++) {
+                                acc[t][x] = T::mfma(vf, p_hi[t], acc[t][x]);
+                                acc[t][x] = T::mfma(vf, p_lo[t], acc[t][x]);
+                            }
+                        } else {
+                            // lane (m, g) adds dimensions 4 g + i of column m
+                            for (int from = 0; from < 4; from++)
+#pragma unroll
+                                for (int j = 0; j < 8; j++)
+#pragma unroll
+                                    for (int i = 0; i < 4; i++) {
+                                        const uint32_t w = (uint32_t)__shfl((int)vf[j >> 1], from * 16 + g * 4 + i, 64);
+                                        const float val = (j & 1) ? T::hi(w) : T::lo(w);
+#pragma unroll
+                                        for (int t = 0; t < kTiles; t++) {
+                                            const float pw = __shfl(s[t][j >> 2][j & 3], from * 16 + m, 64);
+                                            if (pw != 0.0f) acc[t][x][i] += pw * val;
+                                        }
+                                    }
+                        }
+                    }
+                }
+        }
+        if (careful) break;
+        bool odd = false;
+#pragma unroll
+        for (int t = 0; t < kTiles; t++)
+#pragma unroll
+            for (int x = 0; x < kOut; x++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) odd = odd || !(fabsf(acc[t][x][e]) < __builtin_inff());
+        if (!__any(odd)) break;
+        careful = true;
+    }
+
+    // join the waves, in their order
+#pragma unroll
+    for (int t = 0; t < kTiles; t++) {
+        sum[t] += __shfl_xor(sum[t], 16, 64);
+        sum[t] += __shfl_xor(sum[t], 32, 64);
+        if (g == 0) {
+            sm_m[wave][t * 16 + m] = mx[t];
+            sm_l[wave][t * 16 + m] = sum[t];
+        }
+    }
+    __syncthreads();
+    float f[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; t++) {
+        float top = sm_m[0][t * 16 + m];
+#pragma unroll
+        for (int w = 1; w < 4; w++) top = fmaxf(top, sm_m[w][t * 16 + m]);
+        f[t] = __builtin_amdgcn_exp2f(mx[t] - finite_or_zero(top));
+    }
+    for (int w = 0; w < 4; w++) {
+        if (wave == w) {
+#pragma unroll
+            for (int t = 0; t < kTiles; t++)
+#pragma unroll
+                for (int x = 0; x < kOut; x++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int d = (x / kVd) * 128 + (g * 4 + e) * kVd + x % kVd;
+                        float *at = &sm_o[(t * 16 + m) * kPitch + d];
+                        // a wave without tokens has f = 0 and sums of zeros
+                        const float val = acc[t][x][e] * f[t];
+                        *at = w ? *at + val : val;
+                    }
+        }
+        __syncthreads();
+    }
+    const uint32_t rows_here = query_rows - tile * kRows < (uint32_t)kRows ? query_rows - tile * kRows : kRows;
+    for (uint32_t i = threadIdx.x; i < rows_here * (kDim / 4); i += 256) {
+        const uint32_t rr = i / (kDim / 4), d = i % (kDim / 4) * 4;
+        float top = sm_m[0][rr], l = 0.0f;
+#pragma unroll
+        for (int w = 1; w < 4; w++) top = fmaxf(top, sm_m[w][rr]);
+#pragma unroll
+        for (int w = 0; w < 4; w++) l += sm_l[w][rr] * __builtin_amdgcn_exp2f(sm_m[w][rr] - finite_or_zero(top));
+        floatx4 o = *reinterpret_cast<const floatx4 *>(&sm_o[rr * kPitch + d]);
+        if (a.part_o) {
+            const uint64_t at = ((uint64_t)unit * a.n_splits + split) * a.part_rows + rr;
+            *reinterpret_cast<floatx4 *>(a.part_o + at * kDim + d) = o;
+            if (d == 0) *reinterpret_cast<floatx2 *>(a.part_ml + 2 * at) = floatx2{top, l};
+        } else if (d < c.dim) {
+            const float inv = l == 0.0f ? 0.0f : (kE4m3 && c.v_scale ? c.v_scale[head] : 1.0f) / l;
+            const uint32_t r = tile * kRows + rr, tok = r / a.group, h = r % a.group;
+            uint16_t *to = static_cast<uint16_t *>(a.out) +
+                           (((uint64_t)row * a.tokens + tok) * c.n_kv * a.group + (uint64_t)head * a.group + h) * c.dim + d;
+            *reinterpret_cast<uintx2 *>(to) = uintx2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+        }
+    }
+}
+
+template <typename T, bool kE4m3, int kDim, int kTiles>
+hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
+{
+    const uint64_t grid = (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles * a.n_splits;
+    if (a.c.page_size % 16 == 0)
+        attend_kernel<T, kE4m3, kDim, kTiles, true><<<(uint32_t)grid, 256, 0, s>>>(a);
+    else
+        attend_kernel<T, kE4m3, kDim, kTiles, false><<<(uint32_t)grid, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, bool kE4m3>
+hipError_t attend(const DecodeArgs &a, hipStream_t s)
+{
+    const uint32_t dim = padded_dim(a.c.dim), tiles = unit_tiles(a.c.dim, a.group * a.tokens);
+    if (dim == 64) return tiles == 1 ? attend_page<T, kE4m3, 64, 1>(a, s) : attend_page<T, kE4m3, 64, 2>(a, s);
+    if (dim == 128) return tiles == 1 ? attend_page<T, kE4m3, 128, 1>(a, s) : attend_page<T, kE4m3, 128, 2>(a, s);
+    return attend_page<T, kE4m3, 256, 1>(a, s);
+}
+
+}  // namespace ds

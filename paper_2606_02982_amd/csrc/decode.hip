@@ -1,0 +1,226 @@
+// Attention over the paged cache: the split over the cache's length, the join
+// of the splits, the weight per cached token, and the checks of the device
+// data. The attention itself is in attend.h.
+#include "attend.h"
+#include "kernels.h"
+
+namespace ds {
+
+constexpr uint32_t kTargetGroups = 1024;   // workgroups of a launch, where the cache is long enough
+constexpr uint32_t kMinSplitBlocks = 8;    // two blocks per wave
+constexpr uint32_t kMassTokens = 1024;     // tokens of one workgroup of the weights' sum
+constexpr uint32_t kMaxQueryRows = DS_MAX_QUERY_ROWS;
+
+void decode_plan(DecodeArgs &a)
+{
+    const uint32_t query_rows = a.group * a.tokens, unit_rows = 16 * unit_tiles(a.c.dim, query_rows);
+    a.n_tiles = (uint32_t)cdiv(query_rows, unit_rows);
+    a.part_rows = a.n_tiles == 1 ? query_rows : unit_rows;
+    uint64_t blocks = cdiv(a.c.cap, kBlockTokens);
+    if (a.window) {
+        const uint64_t seen = cdiv(a.sinks, kBlockTokens) + cdiv((uint64_t)a.window + a.tokens + kBlockTokens - 2, kBlockTokens);
+        blocks = blocks < seen ? blocks : seen;
+    }
+    a.score_len = (uint32_t)blocks * kBlockTokens;
+    const uint64_t units = (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles;
+    uint64_t per = align_up(cdiv(units * blocks, kTargetGroups), 4);
+    if (per < kMinSplitBlocks) per = kMinSplitBlocks;
+    a.split_blocks = (uint32_t)per;
+    a.n_splits = (uint32_t)cdiv(blocks, per);
+}
+
+static uint64_t part_rows_of(const DecodeArgs &a)
+{
+    return (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles * a.n_splits * a.part_rows;
+}
+
+size_t decode_ws_bytes(const DecodeArgs &a, bool with_mass)
+{
+    size_t b = 0;
+    if (a.n_splits > 1 || with_mass) {
+        b += align_up(part_rows_of(a) * padded_dim(a.c.dim) * 4, 256) + align_up(part_rows_of(a) * 8, 256);
+        if (with_mass) b += align_up((uint64_t)a.n_rows * a.c.n_kv * a.group * a.tokens * a.score_len * 4, 256);
+    }
+    return b;
+}
+
+// Of query row r of (row, head): where its partial results begin, and how far
+// apart the splits lie, in query rows.
+__device__ inline uint64_t part_at(const DecodeArgs &a, uint32_t row, uint32_t head, uint32_t r, uint32_t unit_rows,
+                                   uint64_t &stride)
+{
+    const uint64_t unit = ((uint64_t)row * a.c.n_kv + head) * a.n_tiles + r / unit_rows;
+    stride = a.part_rows;
+    return unit * a.n_splits * a.part_rows + r % unit_rows;
+}
+
+__device__ inline uint32_t length_of(const DecodeArgs &a, uint32_t row, uint32_t &req)
+{
+    req = a.rows ? a.rows[row] : row;
+    const uint32_t n = req < a.c.n_requests ? a.c.len[req] : 0;
+    return n < a.c.cap ? n : a.c.cap;
+}
+
+// Maximum and sum over the splits of one query row, by one wave.
+__device__ inline floatx2 join_ml(const DecodeArgs &a, uint64_t at, uint64_t stride, uint32_t splits)
+{
+    float top = -__builtin_inff(), l = 0.0f;
+    for (uint32_t s = lane_id(); s < splits; s += 64) top = fmaxf(top, a.part_ml[2 * (at + s * stride)]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    for (uint32_t s = lane_id(); s < splits; s += 64) {
+        const floatx2 x = *reinterpret_cast<const floatx2 *>(a.part_ml + 2 * (at + s * stride));
+        l += x[1] * __builtin_amdgcn_exp2f(x[0] - finite_or_zero(top));
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    return floatx2{top, l};
+}
+
+// The first join_groups workgroups join the splits of four query rows each;
+// the others sum the weights of kMassTokens tokens of one (row, head).
+template <typename T, int kDim>
+__global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t join_groups, uint32_t mass_groups,
+                                                   uint32_t unit_rows)
+{
+    constexpr int kPer = kDim / 64;
+    const KvView &c = a.c;
+    const uint32_t query_rows = a.group * a.tokens;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (blockIdx.x < join_groups) {
+        const uint64_t id = (uint64_t)blockIdx.x * 4 + wave;
+        if (id >= (uint64_t)a.n_rows * c.n_kv * query_rows) return;
+        const uint32_t r = (uint32_t)(id % query_rows), head = (uint32_t)(id / query_rows % c.n_kv);
+        const uint32_t row = (uint32_t)(id / query_rows / c.n_kv);
+        uint32_t req;
+        const uint32_t n = length_of(a, row, req);
+        const Span span = span_of(n, a.tokens, a.window, a.sinks);
+        const uint32_t splits = span.total ? (span.total + a.split_blocks - 1) / a.split_blocks : 1;
+        uint64_t stride;
+        const uint64_t at = part_at(a, row, head, r, unit_rows, stride);
+        const floatx2 ml = join_ml(a, at, stride, splits);
+        float o[kPer];
+#pragma unroll
+        for (int k = 0; k < kPer; k++) o[k] = 0.0f;
+        const float *from = a.part_o + at * kDim + lane_id() * kPer;
+        const float base = finite_or_zero(ml[0]);
+#pragma unroll 8
+        for (uint32_t s = 0; s < splits; s++) {
+            const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * (at + s * stride)] - base);
+#pragma unroll
+            for (int k = 0; k < kPer; k++) o[k] += f * from[s * stride * kDim + k];
+        }
+        const float inv = ml[1] == 0.0f ? 0.0f : (c.type == DS_E4M3 && c.v_scale ? c.v_scale[head] : 1.0f) / ml[1];
+        const uint32_t tok = r / a.group, h = r % a.group;
+        uint16_t *to = static_cast<uint16_t *>(a.out) +
+                       (((uint64_t)row * a.tokens + tok) * c.n_kv * a.group + (uint64_t)head * a.group + h) * c.dim;
+#pragma unroll
+        for (int k = 0; k < kPer; k++) {
+            const uint32_t d = lane_id() * kPer + k;
+            if (d < c.dim) to[d] = (uint16_t)T::pack(o[k] * inv, 0.0f);
+        }
+        return;
+    }
+    __shared__ float sm_m[kMaxQueryRows], sm_inv[kMaxQueryRows];
+    const uint32_t id = blockIdx.x - join_groups;
+    const uint32_t chunk = id % mass_groups, head = id / mass_groups % c.n_kv, row = id / mass_groups / c.n_kv;
+    uint32_t req;
+    const uint32_t n = length_of(a, row, req);
+    const Span span = span_of(n, a.tokens, a.window, a.sinks);
+    if (chunk * (kMassTokens / kBlockTokens) >= span.total) return;
+    const uint32_t splits = (span.total + a.split_blocks - 1) / a.split_blocks;
+    for (uint32_t r = wave; r < query_rows; r += 4) {
+        uint64_t stride;
+        const uint64_t at = part_at(a, row, head, r, unit_rows, stride);
+        const floatx2 ml = join_ml(a, at, stride, splits);
+        if (lane_id() == 0) {
+            sm_m[r] = finite_or_zero(ml[0]);
+            sm_inv[r] = ml[1] == 0.0f ? 0.0f : 1.0f / ml[1];
+        }
+    }
+    __syncthreads();
+    const uint32_t tok = chunk * kMassTokens + threadIdx.x * 4, v = tok / kBlockTokens;
+    if (v >= span.total) return;
+    const uint32_t b = v < span.sink_blocks ? v : span.first_block + (v - span.sink_blocks);
+    const uint32_t j = b * kBlockTokens + tok % kBlockTokens;
+    const float *from = a.scores + ((uint64_t)row * c.n_kv + head) * query_rows * a.score_len + tok;
+    floatx4 w = {0, 0, 0, 0};
+    for (uint32_t r = 0; r < query_rows; r++) {
+        const floatx4 s = *reinterpret_cast<const floatx4 *>(from + (uint64_t)r * a.score_len);
+#pragma unroll
+        for (int e = 0; e < 4; e++) w[e] += __builtin_amdgcn_exp2f(s[e] - sm_m[r]) * sm_inv[r];
+    }
+    float *to = a.mass + ((uint64_t)req * c.n_kv + head) * a.mass_len + j;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (j + e < n) to[e] = j + e + a.tokens < n ? to[e] + w[e] : w[e];
+}
+
+template <typename T>
+static hipError_t join(const DecodeArgs &a, hipStream_t s)
+{
+    const uint32_t query_rows = a.group * a.tokens, unit_rows = 16 * unit_tiles(a.c.dim, query_rows);
+    const uint32_t groups = (uint32_t)cdiv((uint64_t)a.n_rows * a.c.n_kv * query_rows, 4);
+    const uint32_t mass_groups = a.mass ? (uint32_t)cdiv(a.score_len, kMassTokens) : 0;
+    const uint32_t grid = groups + a.n_rows * a.c.n_kv * mass_groups;
+    const uint32_t dim = padded_dim(a.c.dim);
+    if (dim == 64)
+        join_kernel<T, 64><<<grid, 256, 0, s>>>(a, groups, mass_groups, unit_rows);
+    else if (dim == 128)
+        join_kernel<T, 128><<<grid, 256, 0, s>>>(a, groups, mass_groups, unit_rows);
+    else
+        join_kernel<T, 256><<<grid, 256, 0, s>>>(a, groups, mass_groups, unit_rows);
+    return hipGetLastError();
+}
+
+hipError_t decode_launch(DecodeArgs a, void *ws, hipStream_t s)
+{
+    a.part_o = a.part_ml = a.scores = nullptr;
+    if (a.n_splits > 1 || a.mass) {
+        uint8_t *p = static_cast<uint8_t *>(ws);
+        a.part_o = reinterpret_cast<float *>(p);
+        p += align_up(part_rows_of(a) * padded_dim(a.c.dim) * 4, 256);
+        a.part_ml = reinterpret_cast<float *>(p);
+        p += align_up(part_rows_of(a) * 8, 256);
+        if (a.mass) a.scores = reinterpret_cast<float *>(p);
+    }
+    const bool bf16 = a.q_type == DS_BF16, e4m3 = a.c.type == DS_E4M3;
+    hipError_t e = e4m3 ? (bf16 ? decode_attend_bf16_e4m3(a, s) : decode_attend_f16_e4m3(a, s))
+                        : (bf16 ? decode_attend_bf16(a, s) : decode_attend_f16(a, s));
+    if (e != hipSuccess || !a.part_o) return e;
+    return bf16 ? join<Bf16>(a, s) : join<F16>(a, s);
+}
+
+// Contract of the batch: requests in range (once each, where the call writes
+// per request), lengths and pages in range.
+__global__ void cache_check_kernel(const KvView c, const uint32_t *rows, uint32_t n_rows, bool once, uint32_t *flag)
+{
+    for (uint32_t i = blockIdx.x; i < n_rows; i += gridDim.x) {
+        const uint32_t req = rows ? rows[i] : i;
+        if (req >= c.n_requests) {
+            if (threadIdx.x == 0) atomicOr(flag, 1u);
+            continue;
+        }
+        const uint32_t n = c.len[req];
+        bool bad = n > c.cap;
+        const uint32_t pages = (uint32_t)cdiv(n < c.cap ? n : c.cap, c.page_size);
+        for (uint32_t p = threadIdx.x; p < pages; p += blockDim.x)
+            bad = bad || c.table[(uint64_t)req * c.max_pages + p] >= c.n_pages;
+        if (once && rows)
+            for (uint32_t k = threadIdx.x; k < i; k += blockDim.x) bad = bad || rows[k] == req;
+        if (bad) atomicOr(flag, 1u);
+    }
+}
+
+hipError_t cache_check(const KvView &c, const uint32_t *rows, uint32_t n_rows, bool once, uint32_t *flag, hipStream_t s)
+{
+    cache_check_kernel<<<n_rows < 4096 ? n_rows : 4096, 256, 0, s>>>(c, rows, n_rows, once, flag);
+    return hipGetLastError();
+}
+
+hipError_t decode_check(const DecodeArgs &a, uint32_t *flag, hipStream_t s)
+{
+    return cache_check(a.c, a.rows, a.n_rows, a.mass != nullptr, flag, s);
+}
+
+}  // namespace ds

@@ -1,4 +1,5 @@
-"""Python binding of the DriftSched C ABI (include/driftsched.h).
+"""Python binding of the DriftSched C ABI (include/driftsched.h and, for the
+decode step, include/driftsched_serve.h).
 
 Argument marshalling only: every step runs in the HIP library
 ``libdriftsched.so``. Arrays are torch tensors on the current HIP device;
@@ -51,6 +52,34 @@ class OrderParams(ctypes.Structure):
                 ("weighted_mode", ctypes.c_uint32)]
 
 
+class KvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("n_requests", ctypes.c_uint32), ("max_pages", ctypes.c_uint32), ("n_pages", ctypes.c_uint32),
+                ("page_size", ctypes.c_uint32), ("n_kv", ctypes.c_uint32), ("head_dim", ctypes.c_uint32),
+                ("page_stride", ctypes.c_uint64), ("token_stride", ctypes.c_uint64),
+                ("head_stride", ctypes.c_uint64), ("type", ctypes.c_int)]
+
+
+class DecodeParams(ctypes.Structure):
+    _fields_ = [("n_q", ctypes.c_uint32), ("n_tokens", ctypes.c_uint32), ("q_type", ctypes.c_int),
+                ("q_row_stride", ctypes.c_uint64), ("q_token_stride", ctypes.c_uint64),
+                ("q_head_stride", ctypes.c_uint64), ("scale", ctypes.c_double), ("window", ctypes.c_uint32),
+                ("sinks", ctypes.c_uint32), ("max_len", ctypes.c_uint32), ("mass_len", ctypes.c_uint64)]
+
+
+class EvictParams(ctypes.Structure):
+    _fields_ = [("sinks", ctypes.c_uint32), ("recent", ctypes.c_uint32), ("slack", ctypes.c_uint32),
+                ("max_len", ctypes.c_uint32), ("mass_len", ctypes.c_uint64), ("kept_len", ctypes.c_uint64)]
+
+
+class VerifyParams(ctypes.Structure):
+    _fields_ = [("n_drafts", ctypes.c_uint32), ("vocab", ctypes.c_uint32), ("n_requests", ctypes.c_uint32),
+                ("type", ctypes.c_int), ("target_row_stride", ctypes.c_uint64),
+                ("target_pos_stride", ctypes.c_uint64), ("draft_row_stride", ctypes.c_uint64),
+                ("draft_pos_stride", ctypes.c_uint64)]
+
+
 class SimParams(ctypes.Structure):
     _fields_ = [("policy", ctypes.c_int), ("batch", ctypes.c_uint32), ("alpha", ctypes.c_double),
                 ("score", ScoreParams), ("order", OrderParams)]
@@ -83,6 +112,14 @@ def _load():
     lib.ds_simulate_multi.argtypes = [u32, u32, P, P, P, P, P, P, P, P, u32, P, u32, u32, P, u32,
                                       ctypes.POINTER(SimParams), ctypes.POINTER(P), ctypes.POINTER(P),
                                       ctypes.POINTER(P), P, P, sz, u32, P]
+    lib.ds_decode_attention.argtypes = [P, P, u32, P, P, P, P, P, sz, u32, P]
+    lib.ds_cache_evict.argtypes = [P, P, P, u32, P, P, P, P, P, P, sz, u32, P]
+    lib.ds_verify_draft.argtypes = [P, u32, P, P, P, P, P, P, P, P, P, P, P, P, sz, u32, P]
+    lib.ds_decode_workspace_bytes.argtypes = [P, P, u32, i32]
+    lib.ds_verify_workspace_bytes.argtypes = [P, u32]
+    lib.ds_decode_workspace_bytes.restype = lib.ds_verify_workspace_bytes.restype = sz
+    for f in (lib.ds_decode_attention, lib.ds_cache_evict, lib.ds_verify_draft):
+        f.restype = i32
     for f in (lib.ds_characterize, lib.ds_characterize_score, lib.ds_characterize_score_noalloc,
               lib.ds_calibrate, lib.ds_calibrate_ex, lib.ds_score, lib.ds_order,
               lib.ds_order_multi, lib.ds_error_stats, lib.ds_class_histogram, lib.ds_simulate,
@@ -529,3 +566,218 @@ def simulate_multi(arrival, tier, counts, category, tenant, group, observed, t_b
                                  _ptr(tick_t), tick_t.numel(), pa, st_p, sq_p, tk_p, _ptr(nd),
                                  _ptr(ws), ws.numel(), _flags(validate), _stream()))
     return outs, nd
+
+
+# ---- the decode step of a dispatched batch (include/driftsched_serve.h) ------------
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+
+
+def _on(device, **tensors):
+    """Device and type of a call's tensors: every one on ``device``, which is
+    the current one (the stream is torch's current stream there)."""
+    if device.type != "cuda":
+        raise ValueError("the tensors must be device tensors")
+    if device.index != torch.cuda.current_device():
+        raise ValueError("the tensors are on %s, which is not the current device" % device)
+    for name, (t, dtype) in tensors.items():
+        if t is None:
+            continue
+        if t.device != device:
+            raise ValueError("%s must be on %s" % (name, device))
+        if t.dtype != dtype:
+            raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+
+
+def _whole(**tensors):
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+
+
+def _shaped(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+
+
+def _scratch(ws, need, device):
+    """The caller's workspace, or one of this call alone: taken from torch's
+    allocator on the current stream, so calls on other streams and in captured
+    graphs share nothing with it."""
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=device) if ws is None else ws
+
+
+class Cache:
+    """A paged key-value cache (``kv_cache``): the tensors and their C struct."""
+
+    def __init__(self, k, v, table, lens, k_scale, v_scale):
+        self.k, self.v, self.table, self.lens = k, v, table, lens
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.device = k.device
+        s = self.struct = KvCache()
+        s.k, s.v, s.table, s.len = k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr()
+        s.k_scale = k_scale.data_ptr() if k_scale is not None else None
+        s.v_scale = v_scale.data_ptr() if v_scale is not None else None
+        s.n_pages, s.page_size, s.n_kv, s.head_dim = k.shape
+        s.n_requests, s.max_pages = table.shape
+        s.page_stride, s.token_stride, s.head_stride = k.stride()[:3]
+        s.type = DTYPES[k.dtype]
+        self.ref = ctypes.byref(s)
+
+
+def kv_cache(k, v, table, lens, k_scale=None, v_scale=None):
+    """A paged key-value cache for ``decode_attention`` and ``cache_evict``.
+
+    ``k``, ``v``: (n_pages, page_size, n_kv, head_dim), float16, bfloat16 or
+    float8_e4m3fn, with the same strides; any order of the first three axes in
+    memory, the last one dense. ``table``: int32 (n_requests, max_pages), the
+    pages of each request in token order. ``lens``: int32 (n_requests), cached
+    tokens. ``k_scale``, ``v_scale``: float32 (n_kv), 8-bit caches only.
+
+    The object keeps the tensors; their contents may change between calls."""
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+        raise ValueError("k and v must be (n_pages, page_size, n_kv, head_dim) of one type and with the same strides")
+    if k.dtype not in DTYPES or k.dtype == torch.float32:
+        raise ValueError("k and v must be float16, bfloat16 or float8_e4m3fn, got %s" % k.dtype)
+    if k.stride(3) != 1:
+        raise ValueError("the last axis of k and v must be dense")
+    if table.dim() != 2:
+        raise ValueError("table must be (n_requests, max_pages)")
+    _shaped(lens, (table.shape[0],), "lens")
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        _shaped(t, (k.shape[2],), name)
+    f32, i32 = torch.float32, torch.int32
+    _on(k.device, v=(v, k.dtype), table=(table, i32), lens=(lens, i32), k_scale=(k_scale, f32), v_scale=(v_scale, f32))
+    _whole(table=table, lens=lens, k_scale=k_scale, v_scale=v_scale)
+    return Cache(k, v, table, lens, k_scale, v_scale)
+
+
+def _mass_of(mass, cache, name):
+    if mass is not None and (mass.dim() != 3 or mass.shape[:2] != (cache.struct.n_requests, cache.struct.n_kv)):
+        raise ValueError("%s must be (n_requests, n_kv, length)" % name)
+
+
+def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len=0, mass=None, out=None, ws=None,
+                     validate=False):
+    """Attention of the newest tokens of a batch over its cache (ds_decode_attention).
+
+    ``q``: (n_rows, n_tokens, n_q, head_dim), the queries of each request's
+    last n_tokens cached tokens, float16 or bfloat16; the last axis dense.
+    ``rows``: int32 (n_rows), the request of each row, e.g. the head of an
+    ``order`` permutation; None: row i is request i. ``scale``: 1 /
+    sqrt(head_dim) by default. ``window``, ``sinks``: tokens seen back (0: all)
+    and first tokens always seen. ``max_len``: the most tokens any request of
+    the batch holds, if known (a tighter launch and workspace). ``mass``:
+    float32 (n_requests, n_kv, length >= max_len), updated in place with the
+    weight each cached token received. Returns out, shaped like q."""
+    if q.dim() != 4 or q.shape[3] != cache.struct.head_dim or q.stride(3) != 1:
+        raise ValueError("q must be (n_rows, n_tokens, n_q, head_dim) with a dense last axis")
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("q must be float16 or bfloat16, got %s" % q.dtype)
+    n, t, h, d = q.shape
+    if out is None:
+        out = torch.empty((n, t, h, d), dtype=q.dtype, device=q.device)
+    _on(cache.device, q=(q, q.dtype), rows=(rows, torch.int32), mass=(mass, torch.float32), out=(out, q.dtype),
+        ws=(ws, torch.uint8))
+    _whole(rows=rows, mass=mass, out=out, ws=ws)
+    _shaped(rows, (n,), "rows")
+    _shaped(out, (n, t, h, d), "out")
+    _mass_of(mass, cache, "mass")
+    p = DecodeParams(h, t, DTYPES[q.dtype], q.stride(0), q.stride(1), q.stride(2),
+                     d ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_len),
+                     mass.shape[2] if mass is not None else 0)
+    ref = ctypes.byref(p)
+    if n:
+        ws = _scratch(ws, lib.ds_decode_workspace_bytes(cache.ref, ref, n, mass is not None), q.device)
+    _check(lib.ds_decode_attention(cache.ref, ref, n, _ptr(rows), _ptr(q), _ptr(out), _ptr(mass), _ptr(ws),
+                                   ws.numel() if ws is not None else 0, _flags(validate), _stream()))
+    return out
+
+
+def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0, max_len=0, mass_out=None, kept=None,
+                ws=None, validate=False):
+    """Requests above their token budget keep the heaviest tokens (ds_cache_evict).
+
+    ``dst``: a ``kv_cache`` of the same layout whose row i names the fresh
+    pages of row i (its k and v may be the pool of ``cache``); ``dst.lens[i]``
+    receives the row's new length, which is smaller than before exactly where
+    the row was cut and copied. ``budget``: float64 (n_requests), e.g. from
+    ``score``. ``mass``: as ``decode_attention`` leaves it. ``mass_out``: None
+    updates mass in place. ``kept``: int32 (n_rows, n_kv, length); by default
+    as long as dst's rows. Returns (dst.lens, kept)."""
+    n = dst.struct.n_requests if rows is None else rows.numel()
+    if mass_out is None:
+        mass_out = mass
+    if kept is None:
+        kept = torch.empty((n, dst.struct.n_kv, dst.struct.max_pages * dst.struct.page_size), dtype=torch.int32,
+                           device=cache.device)
+    f32, i32 = torch.float32, torch.int32
+    _on(cache.device, dst=(dst.k, cache.k.dtype), budget=(budget, torch.float64), mass=(mass, f32), mass_out=(mass_out, f32),
+        kept=(kept, i32), rows=(rows, i32), ws=(ws, torch.uint8))
+    _whole(budget=budget, mass=mass, mass_out=mass_out, kept=kept, rows=rows, ws=ws)
+    _shaped(budget, (cache.struct.n_requests,), "budget")
+    _shaped(rows, (n,), "rows")
+    _mass_of(mass, cache, "mass")
+    _shaped(mass_out, mass.shape, "mass_out")
+    if kept.dim() != 3 or kept.shape[:2] != (n, dst.struct.n_kv):
+        raise ValueError("kept must be (n_rows, n_kv, length)")
+    p = EvictParams(int(sinks), int(recent), int(slack), int(max_len), mass.shape[2], kept.shape[2])
+    if validate:
+        ws = _scratch(ws, 256, cache.device)
+    _check(lib.ds_cache_evict(cache.ref, dst.ref, ctypes.byref(p), n, _ptr(rows), _ptr(budget), _ptr(mass),
+                              _ptr(mass_out), _ptr(kept), _ptr(ws), ws.numel() if ws is not None else 0,
+                              _flags(validate), _stream()))
+    return dst.lens, kept
+
+
+def verify_draft(target, draft, tokens, u, u_sample, n_draft=None, rows=None, observed=None, lens=None, out=None,
+                 n_emitted=None, ws=None, validate=False):
+    """Drafted tokens against the target's probabilities (ds_verify_draft).
+
+    ``target``: (n_rows, n_drafts + 1, vocab) probabilities, float32, float16
+    or bfloat16, the last axis dense; ``draft``: (n_rows, n_drafts, vocab) of
+    the same type, or None for drafts that were not drawn. ``tokens``: int32
+    (n_rows, n_drafts); ``n_draft``: int32 (n_rows) or None. ``u``: float32
+    (n_rows, n_drafts), ``u_sample``: float32 (n_rows), uniform in [0, 1).
+    ``observed``, ``lens``: int32 (n_requests), updated in place at ``rows``.
+    Returns (out, n_emitted): int32 (n_rows, n_drafts + 1) and (n_rows)."""
+    if target.dim() != 3 or target.stride(2) != 1 or target.dtype not in (torch.float32, torch.float16, torch.bfloat16):
+        raise ValueError("target must be (n_rows, n_drafts + 1, vocab), float32, float16 or bfloat16, the last axis dense")
+    n, k, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
+    if k < 0:
+        raise ValueError("target needs at least one position")
+    if draft is not None:
+        _shaped(draft, (n, k, vocab), "draft")
+        if draft.numel() == 0:
+            draft = None
+        elif draft.stride(2) != 1:
+            raise ValueError("the last axis of draft must be dense")
+    dev, i32, f32 = target.device, torch.int32, torch.float32
+    if out is None:
+        out = torch.empty((n, k + 1), dtype=i32, device=dev)
+    if n_emitted is None:
+        n_emitted = torch.empty(n, dtype=i32, device=dev)
+    _on(dev, target=(target, target.dtype), draft=(draft, target.dtype), tokens=(tokens, i32), u=(u, f32),
+        u_sample=(u_sample, f32), n_draft=(n_draft, i32), rows=(rows, i32), observed=(observed, i32), lens=(lens, i32),
+        out=(out, i32), n_emitted=(n_emitted, i32), ws=(ws, torch.uint8))
+    _whole(tokens=tokens, u=u, u_sample=u_sample, n_draft=n_draft, rows=rows, observed=observed, lens=lens, out=out,
+           n_emitted=n_emitted, ws=ws)
+    for t, shape, name in ((tokens, (n, k), "tokens"), (u, (n, k), "u"), (u_sample, (n,), "u_sample"), (rows, (n,), "rows"),
+                           (n_draft, (n,), "n_draft"), (out, (n, k + 1), "out"), (n_emitted, (n,), "n_emitted")):
+        _shaped(t, shape, name)
+    n_req = n
+    for t, name in ((observed, "observed"), (lens, "lens")):
+        if t is not None:
+            n_req = t.numel()
+            _shaped(t, (n_req,), name)
+    if observed is not None and lens is not None:
+        _shaped(lens, observed.shape, "lens")
+    p = VerifyParams(k, vocab, n_req, DTYPES[target.dtype], target.stride(0), target.stride(1),
+                     draft.stride(0) if draft is not None else 0, draft.stride(1) if draft is not None else 0)
+    ref = ctypes.byref(p)
+    if n:
+        ws = _scratch(ws, lib.ds_verify_workspace_bytes(ref, n), dev)
+    _check(lib.ds_verify_draft(ref, n, _ptr(rows), _ptr(target), _ptr(draft), _ptr(tokens), _ptr(n_draft), _ptr(u),
+                               _ptr(u_sample), _ptr(out), _ptr(n_emitted), _ptr(observed), _ptr(lens), _ptr(ws),
+                               ws.numel() if ws is not None else 0, _flags(validate), _stream()))
+    return out, n_emitted
