@@ -80,83 +80,167 @@ struct F16 {
 
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 
-// One workgroup: the tokens of one split for one unit (see DecodeArgs).
-// kDim: padded dimensions; kTiles: 16-row tiles; kPage16: pages hold a
-// multiple of 16 tokens, so that half a block lies in one page and its
-// address is the same for the whole wave.
-template <typename T, bool kE4m3, int kDim, int kTiles, bool kPage16>
-__global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
-{
-    constexpr int kStepsK = kDim / 32;                  // matrix steps per score
-    constexpr int kLoadsK = kE4m3 ? kDim / 64 : kDim / 32;
-    constexpr int kParts = kDim > 128 ? kDim / 128 : 1; // V: pieces of a row
-    constexpr int kVd = kDim / 16 / kParts;             // V: dimensions per lane and piece
-    constexpr int kOut = kDim / 16;                     // 16-dimension tiles of O^T
-    constexpr int kElem = kE4m3 ? 1 : 2;
-    constexpr int kRows = 16 * kTiles;
-    constexpr int kPitch = kDim + 4;
+typedef const __attribute__((address_space(4))) uint32_t *ScalarU32;   // read-only during the launch: scalar loads
 
-    __shared__ float sm_m[4][kRows], sm_l[4][kRows];
-    __shared__ __align__(16) float sm_o[kRows * kPitch];
+// One wave's share of a unit's split: blocks v0 + wave, v0 + wave + 4, ... of
+// the row (see DecodeArgs for units and splits).
+// kDim: padded dimensions; kTiles: 16-row tiles of queries; kFast: all kDim
+// dimensions are there and a page holds a multiple of 16 tokens, so half a
+// block lies in one page, its address is the same for the whole wave, and a
+// lane's place in it is a 32-bit offset. Otherwise addresses are per lane.
+template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast>
+struct Attender {
+    static constexpr int kElem = kE4m3 ? 1 : 2;
+    static constexpr int kStepsK = kDim / 32;                  // matrix steps per score
+    static constexpr int kLoadsK = kE4m3 ? kDim / 64 : kDim / 32;
+    static constexpr int kParts = kDim > 128 ? kDim / 128 : 1; // V: pieces of a row
+    static constexpr int kVd = kDim / 16 / kParts;             // V: dimensions per lane and piece
+    static constexpr int kVw = kVd * kElem / 4;                // V: 32-bit words per lane, token and piece
+    static constexpr int kOut = kDim / 16;                     // 16-dimension tiles of O^T
 
-    const KvView &c = a.c;
-    const int lane = lane_id(), m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const uint32_t split = blockIdx.x % a.n_splits;
-    const uint32_t unit = blockIdx.x / a.n_splits;
-    const uint32_t tile = unit % a.n_tiles;
-    const uint32_t head = unit / a.n_tiles % c.n_kv;
-    const uint32_t row = unit / a.n_tiles / c.n_kv;
-    const uint32_t req = a.rows ? a.rows[row] : row;
-    const uint32_t n_all = req < c.n_requests ? c.len[req] : 0;
-    const uint32_t n = n_all < c.cap ? n_all : c.cap;
-    const Span span = span_of(n, a.tokens, a.window, a.sinks);
-    const uint32_t v0 = split * a.split_blocks;
-    if (split > 0 && v0 >= span.total) return;
-    const uint32_t v1 = v0 + a.split_blocks < span.total ? v0 + a.split_blocks : span.total;
-
-    const uint32_t query_rows = a.group * a.tokens;
-    const int first_pos = (int)n - (int)a.tokens;       // of the first query
-    const int lo = a.window && first_pos >= (int)a.window ? first_pos - (int)a.window + 1 : 0;
-
-    // this lane's queries (one column of each tile)
-    uintx4 q[kTiles][kStepsK];
-    int pos[kTiles];
-#pragma unroll
-    for (int t = 0; t < kTiles; t++) {
-        const uint32_t r = tile * kRows + t * 16 + m;
-        const uint32_t tok = r / a.group, h = r % a.group;
-        pos[t] = r < query_rows ? first_pos + (int)tok : -1;
-        const uint16_t *src = static_cast<const uint16_t *>(a.q) + row * a.q_row + tok * a.q_token +
-                              ((uint64_t)head * a.group + h) * a.q_head;
-#pragma unroll
-        for (int s = 0; s < kStepsK; s++) {
-            const uint32_t d = kE4m3 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
-            q[t][s] = uintx4{0, 0, 0, 0};
-            if (r < query_rows && d < c.dim) q[t][s] = *reinterpret_cast<const uintx4 *>(src + d);
-        }
-    }
-    const float scale = a.scale2 * (kE4m3 && c.k_scale ? c.k_scale[head] : 1.0f);
-    const uint32_t *table = c.table + (uint64_t)req * c.max_pages;
-    const uint8_t *kh = c.k + head * c.head_stride * kElem;
-    const uint8_t *vh = c.v + head * c.head_stride * kElem;
-    float *scores = a.scores;
-
-    auto block_of = [&](uint32_t v) { return v < span.sink_blocks ? v : span.first_block + (v - span.sink_blocks); };
-    // pages of the two halves of block v (kPage16)
-    auto pages_of = [&](uint32_t v, uint32_t *page) {
-        const uint32_t j0 = block_of(v) * kBlockTokens;
-#pragma unroll
-        for (int i = 0; i < 2; i++) page[i] = j0 + 16 * i < n ? table[(j0 + 16 * i) / c.page_size] : 0xFFFFFFFFu;
+    // Where a block's tokens are.
+    struct Place {
+        int j0;
+        uint32_t seen;          // tokens that exist, by bit
+        uint64_t base[2];       // kFast: element offset of each half (the same in all lanes)
+        uint64_t at;            // else: of token (lane & 31)
     };
 
+    const DecodeArgs &a;
+    Span span;
+    uint32_t row, head, tile, query_rows, n;
+    int m, g, first_pos, lo;
+    float scale;
+    ScalarU32 table;
+    const uint8_t *kh, *vh;
+    uint32_t k_lane, v_lane, token_bytes;                      // kFast: this lane's byte offsets
+
+    uintx4 q[kTiles][kStepsK];
+    int pos[kTiles];
     float mx[kTiles], sum[kTiles];
     floatx4 acc[kTiles][kOut];
-    // A pass in which 0 * inf or 0 * NaN of a token that some queries do not
-    // see reached the sums is taken again (careful), with every product made
-    // only where the token is seen.
-    bool careful = false;
-    for (;;) {
+    uintx4 kr[2][kLoadsK];
+    uint32_t vr[8][kParts][kVw];
+
+    __device__ __forceinline__ uint32_t block_of(uint32_t v) const
+    {
+        return v < span.sink_blocks ? v : span.first_block + (v - span.sink_blocks);
+    }
+    __device__ __forceinline__ uint32_t page_of(uint32_t j) const
+    {
+        return a.c.page_shift >= 0 ? j >> a.c.page_shift : j / a.c.page_size;
+    }
+
+    // The pages of block v's halves (kFast; no page where there is no token).
+    __device__ __forceinline__ void pages(uint32_t v, uint32_t v1, uint32_t *page) const
+    {
+        const uint32_t j0 = block_of(v) * kBlockTokens;
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            page[i] = v < v1 && j0 + 16 * i < n ? table[page_of(j0 + 16 * i)] : 0xFFFFFFFFu;
+    }
+
+    __device__ __forceinline__ Place place(uint32_t v, const uint32_t *page) const
+    {
+        Place p;
+        p.j0 = (int)(block_of(v) * kBlockTokens);
+        p.seen = 0xFFFFFFFFu;
+        if constexpr (kFast) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const bool ok = page[i] < a.c.n_pages;
+                if (!ok) p.seen &= i ? 0x0000FFFFu : 0xFFFF0000u;
+                const uint32_t j = (uint32_t)p.j0 + 16 * i, slot = j - page_of(j) * a.c.page_size;
+                p.base[i] = (ok ? page[i] : 0u) * a.c.page_stride + slot * a.c.token_stride;
+            }
+        } else {
+            const uint32_t j = (uint32_t)p.j0 + (lane_id() & 31);
+            const uint32_t pg = j < n ? ((const uint32_t *)a.c.table)[(uint64_t)req * a.c.max_pages + page_of(j)] : 0xFFFFFFFFu;
+            const bool ok = pg < a.c.n_pages;
+            p.seen = (uint32_t)__ballot(ok);
+            p.at = (ok ? pg : 0u) * a.c.page_stride + (j - page_of(j) * a.c.page_size) * a.c.token_stride;
+        }
+        const int left = (int)n - p.j0;
+        if (left < 32) p.seen &= (1u << left) - 1u;
+        return p;
+    }
+    __device__ __forceinline__ uint64_t at_of(const Place &p, int token) const
+    {
+        return ((uint64_t)(uint32_t)__shfl((int)(uint32_t)(p.at >> 32), token, 64) << 32) |
+               (uint32_t)__shfl((int)(uint32_t)p.at, token, 64);
+    }
+
+    __device__ __forceinline__ void load_k(const Place &p)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            if constexpr (kFast) {
+                const uint8_t *base = kh + p.base[i] * kElem;
+#pragma unroll
+                for (int s = 0; s < kLoadsK; s++) kr[i][s] = *reinterpret_cast<const uintx4 *>(base + k_lane + s * 64);
+            } else {
+                const uint8_t *base = kh + at_of(p, 16 * i + m) * kElem;
+#pragma unroll
+                for (int s = 0; s < kLoadsK; s++) {
+                    const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
+                    kr[i][s] = *reinterpret_cast<const uintx4 *>(base + (d < a.c.dim ? d : 0) * kElem);
+                }
+#pragma unroll
+                for (int s = 0; s < kLoadsK; s++) {
+                    const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
+                    if (d >= a.c.dim) kr[i][s] = uintx4{0, 0, 0, 0};
+                }
+            }
+        }
+    }
+
+    // dimensions kVd m .. of each piece, for the lane's eight tokens, as stored
+    __device__ __forceinline__ void load_v(const Place &p)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const uint8_t *base;
+            if constexpr (kFast)
+                base = vh + p.base[j >> 2] * kElem + (j & 3) * token_bytes + v_lane;
+            else
+                base = vh + at_of(p, (j >> 2) * 16 + g * 4 + (j & 3)) * kElem;
+#pragma unroll
+            for (int h = 0; h < kParts; h++) {
+                const uint32_t d = h * 128 + m * kVd;
+                const uint8_t *src = kFast ? base + h * 128 * kElem : base + (d < a.c.dim ? d : 0) * kElem;
+                if constexpr (kVw == 4) {
+                    const uintx4 x = *reinterpret_cast<const uintx4 *>(src);
+#pragma unroll
+                    for (int w = 0; w < 4; w++) vr[j][h][w] = x[w];
+                } else if constexpr (kVw == 2) {
+                    const uintx2 x = *reinterpret_cast<const uintx2 *>(src);
+                    vr[j][h][0] = x[0];
+                    vr[j][h][1] = x[1];
+                } else {
+                    vr[j][h][0] = *reinterpret_cast<const uint32_t *>(src);
+                }
+            }
+        }
+        if constexpr (!kFast)
+#pragma unroll
+            for (int h = 0; h < kParts; h++)
+                if (h * 128 + m * kVd >= (int)a.c.dim)
+#pragma unroll
+                    for (int j = 0; j < 8; j++)
+#pragma unroll
+                        for (int w = 0; w < kVw; w++) vr[j][h][w] = 0;
+    }
+
+    // All blocks of the wave. Keys of the next block are loaded as soon as
+    // the scores have used the present ones, values as soon as the second
+    // product has: while one is waited for the other is under way.
+    // kCareful: 0 * inf or 0 * NaN of a token that some queries do not see
+    // must not reach their sums, so every product is made only where the
+    // weight is not 0 (taken where the first pass gave a number that is not
+    // finite).
+    template <bool kCareful>
+    __device__ __forceinline__ void pass(uint32_t v, uint32_t v1)
+    {
 #pragma unroll
         for (int t = 0; t < kTiles; t++) {
             mx[t] = -__builtin_inff();
@@ -164,96 +248,14 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
 #pragma unroll
             for (int x = 0; x < kOut; x++) acc[t][x] = floatx4{0, 0, 0, 0};
         }
-        uint32_t page[2] = {0, 0};
-        if (kPage16 && v0 + wave < v1) pages_of(v0 + wave, page);
-        for (uint32_t v = v0 + wave; v < v1; v += 4) {
-            const int j0 = (int)(block_of(v) * kBlockTokens);
-            uint32_t seen = 0xFFFFFFFFu;                // tokens of the block that exist, by bit
-            uint64_t k_at[2], v_at[8];                  // element offsets of this lane's tokens
-            if (kPage16) {
-                uint64_t base[2];
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    const bool ok = page[i] < c.n_pages;
-                    if (!ok) seen &= i ? 0x0000FFFFu : 0xFFFF0000u;
-                    const uint32_t slot = (uint32_t)(j0 + 16 * i) % c.page_size;
-                    base[i] = (ok ? page[i] : 0u) * c.page_stride + slot * c.token_stride;
-                    k_at[i] = base[i] + m * c.token_stride;
-                }
-#pragma unroll
-                for (int j = 0; j < 8; j++) v_at[j] = base[j >> 2] + (g * 4 + (j & 3)) * c.token_stride;
-            } else {
-                const uint32_t j = (uint32_t)j0 + (lane & 31);
-                const uint32_t pg = j < n ? table[j / c.page_size] : 0xFFFFFFFFu;
-                const bool ok = pg < c.n_pages;
-                seen = (uint32_t)__ballot(ok);
-                const uint64_t at = (ok ? pg : 0u) * c.page_stride + (j % c.page_size) * c.token_stride;
-                const int lo32 = (int)(uint32_t)at, hi32 = (int)(uint32_t)(at >> 32);
-                auto of = [&](int src) {
-                    return ((uint64_t)(uint32_t)__shfl(hi32, src, 64) << 32) | (uint32_t)__shfl(lo32, src, 64);
-                };
-#pragma unroll
-                for (int i = 0; i < 2; i++) k_at[i] = of(16 * i + m);
-#pragma unroll
-                for (int i = 0; i < 8; i++) v_at[i] = of((i >> 2) * 16 + g * 4 + (i & 3));
-            }
-            uintx4 kr[2][kLoadsK];
-#pragma unroll
-            for (int i = 0; i < 2; i++)
-#pragma unroll
-                for (int s = 0; s < kLoadsK; s++) {
-                    const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
-                    kr[i][s] = uintx4{0, 0, 0, 0};
-                    if (d < c.dim) kr[i][s] = *reinterpret_cast<const uintx4 *>(kh + (k_at[i] + d) * kElem);
-                }
-            // dimensions kVd m .. of part p, for the lane's eight tokens, as
-            // they are stored
-            constexpr int kVw = kVd * kElem / 4;        // 32-bit words per lane, token and part
-            uint32_t vr[8][kParts][kVw];
-#pragma unroll
-            for (int j = 0; j < 8; j++)
-#pragma unroll
-                for (int p = 0; p < kParts; p++) {
-                    const uint32_t d = p * 128 + m * kVd;
-#pragma unroll
-                    for (int w = 0; w < kVw; w++) vr[j][p][w] = 0;
-                    if (d < c.dim) {
-                        const uint8_t *src = vh + (v_at[j] + d) * kElem;
-                        if constexpr (kVw == 4) {
-                            const uintx4 x = *reinterpret_cast<const uintx4 *>(src);
-#pragma unroll
-                            for (int w = 0; w < 4; w++) vr[j][p][w] = x[w];
-                        } else if constexpr (kVw == 2) {
-                            const uintx2 x = *reinterpret_cast<const uintx2 *>(src);
-                            vr[j][p][0] = x[0];
-                            vr[j][p][1] = x[1];
-                        } else {
-                            vr[j][p][0] = *reinterpret_cast<const uint32_t *>(src);
-                        }
-                    }
-                }
-            if (kPage16 && v + 4 < v1) pages_of(v + 4, page);
-
-            // which tokens any query sees; whether every query sees all
-            if ((int)n - j0 < 32) seen &= (1u << ((int)n - j0)) - 1u;
-            const bool full = seen == 0xFFFFFFFFu && j0 + 31 <= first_pos &&
-                              (a.window == 0 || j0 > (int)n - 1 - (int)a.window || j0 + 31 < (int)a.sinks);
-            if (!full) {
-                uint32_t near = 0xFFFFFFFFu;            // at or behind the window's start
-                if (lo > j0) near = lo - j0 < 32 ? ~((1u << (lo - j0)) - 1u) : 0u;
-                uint32_t sink = 0;
-                if ((int)a.sinks > j0) sink = (int)a.sinks - j0 < 32 ? (1u << ((int)a.sinks - j0)) - 1u : 0xFFFFFFFFu;
-                seen &= near | sink;
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const bool on = (seen >> ((j >> 2) * 16 + g * 4 + (j & 3))) & 1u;
-#pragma unroll
-                    for (int p = 0; p < kParts; p++)
-#pragma unroll
-                        for (int w = 0; w < kVw; w++) vr[j][p][w] = on ? vr[j][p][w] : 0u;
-                }
-            }
-
+        if (v >= v1) return;
+        uint32_t page[2];
+        if (kFast) pages(v, v1, page);
+        Place here = place(v, page);
+        load_k(here);
+        load_v(here);
+        if (kFast) pages(v + 4, v1, page);
+        for (;;) {
             floatx4 s[kTiles][2];
 #pragma unroll
             for (int i = 0; i < 2; i++)
@@ -273,6 +275,56 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
                         s[t][i] = T::mfma(kf, q[t][st], s[t][i]);
                     }
                 }
+            const bool more = v + 4 < v1;
+            Place next = here;
+            if (more) {
+                next = place(v + 4, page);
+                load_k(next);
+                if (kFast) pages(v + 8, v1, page);
+            }
+
+            // which tokens any query sees; whether every query sees all
+            uint32_t seen = here.seen;
+            const int j0 = here.j0;
+            const bool full = seen == 0xFFFFFFFFu && j0 + 31 <= first_pos &&
+                              (a.window == 0 || j0 > (int)n - 1 - (int)a.window || j0 + 31 < (int)a.sinks);
+            if (!full) {
+                uint32_t near = 0xFFFFFFFFu;            // at or behind the window's start
+                if (lo > j0) near = lo - j0 < 32 ? ~((1u << (lo - j0)) - 1u) : 0u;
+                uint32_t sink = 0;
+                if ((int)a.sinks > j0) sink = (int)a.sinks - j0 < 32 ? (1u << ((int)a.sinks - j0)) - 1u : 0xFFFFFFFFu;
+                seen &= near | sink;
+#pragma unroll
+                for (int t = 0; t < kTiles; t++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const int bit = 16 * i + g * 4 + e, j = j0 + bit;
+                            const bool on = ((seen >> bit) & 1u) && j <= pos[t] &&
+                                            (a.window == 0 || j > pos[t] - (int)a.window || j < (int)a.sinks);
+                            s[t][i][e] = on ? s[t][i][e] * scale : -__builtin_inff();
+                        }
+            } else {
+#pragma unroll
+                for (int t = 0; t < kTiles; t++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) s[t][i][e] *= scale;
+            }
+            if (a.scores) {
+#pragma unroll
+                for (int t = 0; t < kTiles; t++) {
+                    const uint32_t r = tile * 16 * kTiles + t * 16 + m;
+                    if (r < query_rows) {
+                        float *to = a.scores + (((uint64_t)row * a.c.n_kv + head) * query_rows + r) * a.score_len +
+                                    (uint64_t)v * kBlockTokens + g * 4;
+#pragma unroll
+                        for (int i = 0; i < 2; i++) *reinterpret_cast<floatx4 *>(to + 16 * i) = s[t][i];
+                    }
+                }
+            }
             // softmax step: s becomes the weights
             uintx4 p_hi[kTiles], p_lo[kTiles];
 #pragma unroll
@@ -281,26 +333,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
 #pragma unroll
                 for (int i = 0; i < 2; i++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        float x = s[t][i][e] * scale;
-                        if (!full) {
-                            const int bit = 16 * i + g * 4 + e, j = j0 + bit;
-                            const bool on = ((seen >> bit) & 1u) && j <= pos[t] &&
-                                            (a.window == 0 || j > pos[t] - (int)a.window || j < (int)a.sinks);
-                            x = on ? x : -__builtin_inff();
-                        }
-                        s[t][i][e] = x;
-                        top = fmaxf(top, x);
-                    }
-                if (scores) {
-                    const uint32_t r = tile * kRows + t * 16 + m;
-                    if (r < query_rows) {
-                        float *to = scores + (((uint64_t)row * c.n_kv + head) * query_rows + r) * a.score_len +
-                                    (uint64_t)v * kBlockTokens + g * 4;
-#pragma unroll
-                        for (int i = 0; i < 2; i++) *reinterpret_cast<floatx4 *>(to + 16 * i) = s[t][i];
-                    }
-                }
+                    for (int e = 0; e < 4; e++) top = fmaxf(top, s[t][i][e]);
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
                 if (__any(top > mx[t])) {
@@ -330,27 +363,37 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
                         p_lo[t][i * 2 + e / 2] = T::pack(s[t][i][e] - T::lo(w), s[t][i][e + 1] - T::hi(w));
                     }
             }
+            if (!full) {
 #pragma unroll
-            for (int p = 0; p < kParts; p++)
+                for (int j = 0; j < 8; j++) {
+                    const bool on = (seen >> ((j >> 2) * 16 + g * 4 + (j & 3))) & 1u;
+#pragma unroll
+                    for (int h = 0; h < kParts; h++)
+#pragma unroll
+                        for (int w = 0; w < kVw; w++) vr[j][h][w] = on ? vr[j][h][w] : 0u;
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < kParts; h++)
 #pragma unroll
                 for (int d = 0; d < kVd; d += 2) {
                     uint32_t pair[8];                   // dimensions d, d + 1 of the eight tokens
 #pragma unroll
                     for (int j = 0; j < 8; j++) {
                         if constexpr (kE4m3)
-                            pair[j] = (d & 2) ? T::template from_e4m3<true>(vr[j][p][d >> 2])
-                                              : T::template from_e4m3<false>(vr[j][p][d >> 2]);
+                            pair[j] = (d & 2) ? T::template from_e4m3<true>(vr[j][h][d >> 2])
+                                              : T::template from_e4m3<false>(vr[j][h][d >> 2]);
                         else
-                            pair[j] = vr[j][p][d >> 1];
+                            pair[j] = vr[j][h][d >> 1];
                     }
 #pragma unroll
                     for (int o = 0; o < 2; o++) {
-                        const int x = p * kVd + d + o;
+                        const int x = h * kVd + d + o;
                         const uint32_t sel = o ? 0x07060302u : 0x05040100u;
                         uintx4 vf;
 #pragma unroll
                         for (int w = 0; w < 4; w++) vf[w] = __builtin_amdgcn_perm(pair[2 * w + 1], pair[2 * w], sel);
-                        if (!careful) {
+                        if constexpr (!kCareful) {
 #pragma unroll
                             for (int t = 0; t < kTiles; t++) {
                                 acc[t][x] = T::mfma(vf, p_hi[t], acc[t][x]);
@@ -358,35 +401,112 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
                             }
                         } else {
                             // lane (m, g) adds dimensions 4 g + i of column m
+#pragma unroll 1
                             for (int from = 0; from < 4; from++)
 #pragma unroll
                                 for (int j = 0; j < 8; j++)
 #pragma unroll
-                                    for (int i = 0; i < 4; i++) {
-                                        const uint32_t w = (uint32_t)__shfl((int)vf[j >> 1], from * 16 + g * 4 + i, 64);
-                                        const float val = (j & 1) ? T::hi(w) : T::lo(w);
+                                    for (int t = 0; t < kTiles; t++) {
+                                        const float pw = __shfl(s[t][j >> 2][j & 3], from * 16 + m, 64);
 #pragma unroll
-                                        for (int t = 0; t < kTiles; t++) {
-                                            const float pw = __shfl(s[t][j >> 2][j & 3], from * 16 + m, 64);
+                                        for (int i = 0; i < 4; i++) {
+                                            const uint32_t w = (uint32_t)__shfl((int)vf[j >> 1], from * 16 + g * 4 + i, 64);
+                                            const float val = (j & 1) ? T::hi(w) : T::lo(w);
                                             if (pw != 0.0f) acc[t][x][i] += pw * val;
                                         }
                                     }
                         }
                     }
                 }
+            if (!more) break;
+            here = next;
+            load_v(here);
+            v += 4;
         }
-        if (careful) break;
-        bool odd = false;
+    }
+    uint32_t req;
+};
+
+template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast>
+__global__ __launch_bounds__(256, (kDim * kTiles <= 64    ? 4
+                                   : kDim * kTiles <= 128 ? (kFast ? 3 : 2)
+                                   : kDim <= 128          ? (kFast ? 2 : 1)
+                                                          : 1))
+void attend_kernel(const DecodeArgs a)
+{
+    typedef Attender<T, kE4m3, kDim, kTiles, kFast> A;
+    constexpr int kRows = 16 * kTiles;
+    constexpr int kPitch = kDim + 4;
+
+    __shared__ float sm_m[4][kRows], sm_l[4][kRows];
+    __shared__ __align__(16) float sm_o[kRows * kPitch];
+
+    const KvView &c = a.c;
+    const int lane = lane_id(), m = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const uint32_t split = blockIdx.x % a.n_splits;
+    const uint32_t unit = blockIdx.x / a.n_splits;
+    const uint32_t tile = unit % a.n_tiles;
+    const uint32_t head = unit / a.n_tiles % c.n_kv;
+    const uint32_t row = unit / a.n_tiles / c.n_kv;
+    const uint32_t req = a.rows ? ((ScalarU32)(uint64_t)a.rows)[row] : row;
+    const uint32_t n_all = req < c.n_requests ? ((ScalarU32)(uint64_t)c.len)[req] : 0;
+    const uint32_t n = n_all < c.cap ? n_all : c.cap;
+    const Span span = span_of(n, a.tokens, a.window, a.sinks);
+    const uint32_t v0 = split * a.split_blocks;
+    if (split > 0 && v0 >= span.total) return;
+    const uint32_t v1 = v0 + a.split_blocks < span.total ? v0 + a.split_blocks : span.total;
+    const uint32_t query_rows = a.group * a.tokens;
+    const int first_pos = (int)n - (int)a.tokens;       // of the first query
+
+    A w{a};
+    w.span = span;
+    w.row = row;
+    w.req = req;
+    w.head = head;
+    w.tile = tile;
+    w.query_rows = query_rows;
+    w.n = n;
+    w.m = m;
+    w.g = g;
+    w.first_pos = first_pos;
+    w.lo = a.window && first_pos >= (int)a.window ? first_pos - (int)a.window + 1 : 0;
+    w.scale = a.scale2 * (kE4m3 && c.k_scale ? c.k_scale[head] : 1.0f);
+    w.table = (ScalarU32)(uint64_t)(c.table + (uint64_t)req * c.max_pages);
+    w.kh = c.k + head * c.head_stride * A::kElem;
+    w.vh = c.v + head * c.head_stride * A::kElem;
+    w.token_bytes = (uint32_t)c.token_stride * A::kElem;
+    w.k_lane = m * w.token_bytes + g * 16;
+    w.v_lane = g * 4 * w.token_bytes + m * A::kVd * A::kElem;
+    // this lane's queries (one column of each tile)
 #pragma unroll
-        for (int t = 0; t < kTiles; t++)
+    for (int t = 0; t < kTiles; t++) {
+        const uint32_t r = tile * kRows + t * 16 + m;
+        const uint32_t tok = r / a.group, h = r % a.group;
+        w.pos[t] = r < query_rows ? first_pos + (int)tok : -1;
+        const uint16_t *src = static_cast<const uint16_t *>(a.q) + row * a.q_row + tok * a.q_token +
+                              ((uint64_t)head * a.group + h) * a.q_head;
 #pragma unroll
-            for (int x = 0; x < kOut; x++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) odd = odd || !(fabsf(acc[t][x][e]) < __builtin_inff());
-        if (!__any(odd)) break;
-        careful = true;
+        for (int s = 0; s < A::kStepsK; s++) {
+            const uint32_t d = kE4m3 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+            w.q[t][s] = uintx4{0, 0, 0, 0};
+            if (r < query_rows && d < c.dim) w.q[t][s] = *reinterpret_cast<const uintx4 *>(src + d);
+        }
     }
 
+    w.template pass<false>(v0 + wave, v1);
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < kTiles; t++)
+#pragma unroll
+        for (int x = 0; x < A::kOut; x++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) odd = odd || !(fabsf(w.acc[t][x][e]) < __builtin_inff());
+    if (__any(odd)) w.template pass<true>(v0 + wave, v1);
+    auto &mx = w.mx;
+    auto &sum = w.sum;
+    auto &acc = w.acc;
+    constexpr int kOut = A::kOut, kVd = A::kVd;
     // join the waves, in their order
 #pragma unroll
     for (int t = 0; t < kTiles; t++) {
@@ -403,11 +523,11 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
     for (int t = 0; t < kTiles; t++) {
         float top = sm_m[0][t * 16 + m];
 #pragma unroll
-        for (int w = 1; w < 4; w++) top = fmaxf(top, sm_m[w][t * 16 + m]);
+        for (int k = 1; k < 4; k++) top = fmaxf(top, sm_m[k][t * 16 + m]);
         f[t] = __builtin_amdgcn_exp2f(mx[t] - finite_or_zero(top));
     }
-    for (int w = 0; w < 4; w++) {
-        if (wave == w) {
+    for (int k = 0; k < 4; k++) {
+        if (wave == k) {
 #pragma unroll
             for (int t = 0; t < kTiles; t++)
 #pragma unroll
@@ -418,7 +538,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
                         float *at = &sm_o[(t * 16 + m) * kPitch + d];
                         // a wave without tokens has f = 0 and sums of zeros
                         const float val = acc[t][x][e] * f[t];
-                        *at = w ? *at + val : val;
+                        *at = k ? *at + val : val;
                     }
         }
         __syncthreads();
@@ -428,9 +548,9 @@ __global__ __launch_bounds__(256) void attend_kernel(const DecodeArgs a)
         const uint32_t rr = i / (kDim / 4), d = i % (kDim / 4) * 4;
         float top = sm_m[0][rr], l = 0.0f;
 #pragma unroll
-        for (int w = 1; w < 4; w++) top = fmaxf(top, sm_m[w][rr]);
+        for (int k = 1; k < 4; k++) top = fmaxf(top, sm_m[k][rr]);
 #pragma unroll
-        for (int w = 0; w < 4; w++) l += sm_l[w][rr] * __builtin_amdgcn_exp2f(sm_m[w][rr] - finite_or_zero(top));
+        for (int k = 0; k < 4; k++) l += sm_l[k][rr] * __builtin_amdgcn_exp2f(sm_m[k][rr] - finite_or_zero(top));
         floatx4 o = *reinterpret_cast<const floatx4 *>(&sm_o[rr * kPitch + d]);
         if (a.part_o) {
             const uint64_t at = ((uint64_t)unit * a.n_splits + split) * a.part_rows + rr;
@@ -450,7 +570,8 @@ template <typename T, bool kE4m3, int kDim, int kTiles>
 hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
 {
     const uint64_t grid = (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles * a.n_splits;
-    if (a.c.page_size % 16 == 0)
+    // lane offsets in half a block take 32 bits
+    if (a.c.page_size % 16 == 0 && a.c.dim == kDim && a.c.token_stride < (1u << 26))
         attend_kernel<T, kE4m3, kDim, kTiles, true><<<(uint32_t)grid, 256, 0, s>>>(a);
     else
         attend_kernel<T, kE4m3, kDim, kTiles, false><<<(uint32_t)grid, 256, 0, s>>>(a);

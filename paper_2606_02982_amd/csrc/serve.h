@@ -18,6 +18,7 @@ struct KvView {
     uint32_t n_requests, max_pages, n_pages, page_size, n_kv, dim, cap;
     uint64_t page_stride, token_stride, head_stride;   // elements
     int type;
+    int page_shift;        // log2(page_size), or -1
 };
 
 struct DecodeArgs {

@@ -45,6 +45,7 @@ ds_status view_of(const ds_kv_cache *c, uint32_t max_len, KvView &v)
     v.token_stride = c->token_stride;
     v.head_stride = c->head_stride;
     v.type = type;
+    v.page_shift = c->page_size & (c->page_size - 1) ? -1 : __builtin_ctz(c->page_size);
     return DS_OK;
 }
 
