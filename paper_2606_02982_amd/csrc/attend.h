@@ -82,8 +82,92 @@ __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builti
 
 typedef const __attribute__((address_space(4))) uint32_t *ScalarU32;   // read-only during the launch: scalar loads
 
-// One wave's share of a unit's split: blocks v0 + wave, v0 + wave + 4, ... of
-// the row (see DecodeArgs for units and splits).
+constexpr uint32_t kMinSlotBlocks = 8;     // two blocks per wave
+constexpr uint32_t kBalancedRows = 1024;   // rows whose lengths every workgroup looks through
+
+__device__ __forceinline__ uint32_t length_of(const DecodeArgs &a, uint32_t row, uint32_t &req)
+{
+    req = a.rows ? a.rows[row] : row;
+    const uint32_t n = req < a.c.n_requests ? a.c.len[req] : 0;
+    return n < a.c.cap ? n : a.c.cap;
+}
+
+struct Slots {
+    uint32_t row;          // kNone: there is no such slot
+    uint32_t first, count; // the row's slots
+    uint32_t req, n;       // its request and length
+};
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+// The row that slot `want` belongs to. Rows differ in length, so slots are
+// cut from the batch's blocks as a whole: of all rows' blocks a slot gets at
+// most ceil(blocks / slot_goal), at least kMinSlotBlocks, and a row is cut
+// into equal slots of at most that. Every workgroup of 256 threads finds this
+// by itself, looking through the rows' lengths (a launch before would cost
+// more than the few hundred cycles).
+__device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
+{
+    if (a.slot_goal == 0) {
+        Slots s{want < a.n_rows ? want : kNone, want, 1, 0, 0};
+        if (s.row != kNone) s.n = length_of(a, want, s.req);
+        return s;
+    }
+    __shared__ uint64_t sm_blocks[4];
+    __shared__ uint32_t sm_slots[4], sm_found[5];
+    const uint32_t each = (a.n_rows + 255) / 256, r0 = threadIdx.x * each;
+    const uint32_t r1 = r0 + each < a.n_rows ? r0 + each : a.n_rows;
+    const int wave = threadIdx.x >> 6;
+    uint64_t blocks = 0;
+    uint32_t total = 0, n = 0, req = 0;                 // of the last row looked at
+    auto look = [&](uint32_t r) {
+        n = length_of(a, r, req);
+        total = span_of(n, a.tokens, a.window, a.sinks).total;
+    };
+    for (uint32_t r = r0; r < r1; r++) {
+        look(r);
+        blocks += total;
+    }
+    uint64_t all = blocks;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) all += __shfl_xor(all, d, 64);
+    if (lane_id() == 0) sm_blocks[wave] = all;
+    if (threadIdx.x == 0) sm_found[0] = kNone;
+    __syncthreads();
+    all = sm_blocks[0] + sm_blocks[1] + sm_blocks[2] + sm_blocks[3];
+    // all < 2^37: a float holds the quotient to far less than a slot
+    uint32_t most = (uint32_t)((float)all / (float)a.slot_goal) + 1;
+    most = most > kMinSlotBlocks ? most : kMinSlotBlocks;
+    auto slots_of = [&](uint32_t t) { return t <= most ? 1u : (t + most - 1) / most; };
+    uint32_t own = 0;
+    for (uint32_t r = r0; r < r1; r++) {
+        if (each > 1) look(r);
+        own += slots_of(total);
+    }
+    const uint32_t incl = wave_incl_scan_dpp(own);
+    if (lane_id() == 63) sm_slots[wave] = incl;
+    __syncthreads();
+    uint32_t first = incl - own;
+    for (int w = 0; w < wave; w++) first += sm_slots[w];
+    if (want - first < own)
+        for (uint32_t r = r0; r < r1; r++) {
+            if (each > 1) look(r);
+            const uint32_t count = slots_of(total);
+            if (want - first < count) {
+                sm_found[0] = r;
+                sm_found[1] = first;
+                sm_found[2] = count;
+                sm_found[3] = req;
+                sm_found[4] = n;
+            }
+            first += count;
+        }
+    __syncthreads();
+    auto same = [&](int k) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)sm_found[k]); };
+    return Slots{same(0), same(1), same(2), same(3), same(4)};
+}
+
+// One wave's share of a unit: blocks v0 + wave, v0 + wave + 4, ... of the slot
+// (see DecodeArgs for slots and units).
 // kDim: padded dimensions; kTiles: 16-row tiles of queries; kFast: all kDim
 // dimensions are there and a page holds a multiple of 16 tokens, so half a
 // block lies in one page, its address is the same for the whole wave, and a
@@ -428,7 +512,7 @@ struct Attender {
 };
 
 template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast>
-__global__ __launch_bounds__(256, (kDim * kTiles <= 64    ? 4
+__global__ __launch_bounds__(256, (kDim * kTiles <= 64    ? (kFast ? 4 : 3)
                                    : kDim * kTiles <= 128 ? (kFast ? 3 : 2)
                                    : kDim <= 128          ? (kFast ? 2 : 1)
                                                           : 1))
@@ -444,18 +528,21 @@ void attend_kernel(const DecodeArgs a)
     const KvView &c = a.c;
     const int lane = lane_id(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const uint32_t split = blockIdx.x % a.n_splits;
-    const uint32_t unit = blockIdx.x / a.n_splits;
-    const uint32_t tile = unit % a.n_tiles;
-    const uint32_t head = unit / a.n_tiles % c.n_kv;
-    const uint32_t row = unit / a.n_tiles / c.n_kv;
-    const uint32_t req = a.rows ? ((ScalarU32)(uint64_t)a.rows)[row] : row;
-    const uint32_t n_all = req < c.n_requests ? ((ScalarU32)(uint64_t)c.len)[req] : 0;
-    const uint32_t n = n_all < c.cap ? n_all : c.cap;
+    // units of one pair on one of the eight dies (workgroups go round them):
+    // they read the same keys and values
+    const uint32_t round = blockIdx.x / (8 * a.n_tiles), within = blockIdx.x % (8 * a.n_tiles);
+    const uint32_t tile = within / 8, pair = round * 8 + within % 8;
+    const uint32_t slot = pair / c.n_kv, head = pair % c.n_kv;
+    const Slots slots = find_slots(a, slot);
+    const uint32_t row = slots.row;
+    if (row == kNone) return;
+    const uint32_t req = slots.req, n = slots.n;
+    if (a.row_slots && slot == slots.first && head == 0 && tile == 0 && threadIdx.x == 0)
+        *reinterpret_cast<uintx2 *>(a.row_slots + 2 * row) = uintx2{slots.first, slots.count};
     const Span span = span_of(n, a.tokens, a.window, a.sinks);
-    const uint32_t v0 = split * a.split_blocks;
-    if (split > 0 && v0 >= span.total) return;
-    const uint32_t v1 = v0 + a.split_blocks < span.total ? v0 + a.split_blocks : span.total;
+    const uint32_t per = slots.count == 1 ? span.total : (span.total + slots.count - 1) / slots.count;
+    const uint32_t v0 = (slot - slots.first) * per;
+    const uint32_t v1 = v0 + per < span.total ? v0 + per : span.total;
     const uint32_t query_rows = a.group * a.tokens;
     const int first_pos = (int)n - (int)a.tokens;       // of the first query
 
@@ -552,10 +639,10 @@ void attend_kernel(const DecodeArgs a)
 #pragma unroll
         for (int k = 0; k < 4; k++) l += sm_l[k][rr] * __builtin_amdgcn_exp2f(sm_m[k][rr] - finite_or_zero(top));
         floatx4 o = *reinterpret_cast<const floatx4 *>(&sm_o[rr * kPitch + d]);
-        if (a.part_o) {
-            const uint64_t at = ((uint64_t)unit * a.n_splits + split) * a.part_rows + rr;
+        const uint64_t at = ((uint64_t)pair * a.n_tiles + tile) * a.part_rows + rr;
+        if (a.part_ml && d == 0) *reinterpret_cast<floatx2 *>(a.part_ml + 2 * at) = floatx2{top, l};
+        if (slots.count > 1) {
             *reinterpret_cast<floatx4 *>(a.part_o + at * kDim + d) = o;
-            if (d == 0) *reinterpret_cast<floatx2 *>(a.part_ml + 2 * at) = floatx2{top, l};
         } else if (d < c.dim) {
             const float inv = l == 0.0f ? 0.0f : (kE4m3 && c.v_scale ? c.v_scale[head] : 1.0f) / l;
             const uint32_t r = tile * kRows + rr, tok = r / a.group, h = r % a.group;
@@ -569,7 +656,7 @@ void attend_kernel(const DecodeArgs a)
 template <typename T, bool kE4m3, int kDim, int kTiles>
 hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
 {
-    const uint64_t grid = (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles * a.n_splits;
+    const uint64_t grid = cdiv((uint64_t)a.n_slots * a.c.n_kv, 8) * 8 * a.n_tiles;
     // lane offsets in half a block take 32 bits
     if (a.c.page_size % 16 == 0 && a.c.dim == kDim && a.c.token_stride < (1u << 26))
         attend_kernel<T, kE4m3, kDim, kTiles, true><<<(uint32_t)grid, 256, 0, s>>>(a);

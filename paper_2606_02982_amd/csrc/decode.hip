@@ -6,8 +6,7 @@
 
 namespace ds {
 
-constexpr uint32_t kTargetGroups = 1024;   // workgroups of a launch, where the cache is long enough
-constexpr uint32_t kMinSplitBlocks = 8;    // two blocks per wave
+constexpr uint32_t kPairGoal = 1536;       // pairs of a launch, where the caches are long enough
 constexpr uint32_t kMassTokens = 1024;     // tokens of one workgroup of the weights' sum
 constexpr uint32_t kMaxQueryRows = DS_MAX_QUERY_ROWS;
 
@@ -22,102 +21,99 @@ void decode_plan(DecodeArgs &a)
         blocks = blocks < seen ? blocks : seen;
     }
     a.score_len = (uint32_t)blocks * kBlockTokens;
-    const uint64_t units = (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles;
-    uint64_t per = align_up(cdiv(units * blocks, kTargetGroups), 4);
-    if (per < kMinSplitBlocks) per = kMinSplitBlocks;
-    a.split_blocks = (uint32_t)per;
-    a.n_splits = (uint32_t)cdiv(blocks, per);
+    // no row can be cut, or so many rows that none need be: one slot each
+    a.slot_goal = blocks > kMinSlotBlocks && a.n_rows <= kBalancedRows ? (uint32_t)cdiv(kPairGoal, a.c.n_kv) : 0;
+    a.n_slots = a.n_rows;
+    if (a.slot_goal) {
+        // ceil(total / most) <= total / most + 1 per row
+        const uint64_t most = (uint64_t)a.n_rows * cdiv(blocks, kMinSlotBlocks);
+        a.n_slots = (uint32_t)(a.slot_goal + a.n_rows < most ? a.slot_goal + a.n_rows : most);
+    }
 }
 
-static uint64_t part_rows_of(const DecodeArgs &a)
-{
-    return (uint64_t)a.n_rows * a.c.n_kv * a.n_tiles * a.n_splits * a.part_rows;
-}
+static uint64_t part_rows_of(const DecodeArgs &a) { return (uint64_t)a.n_slots * a.c.n_kv * a.n_tiles * a.part_rows; }
 
 size_t decode_ws_bytes(const DecodeArgs &a, bool with_mass)
 {
     size_t b = 0;
-    if (a.n_splits > 1 || with_mass) {
-        b += align_up(part_rows_of(a) * padded_dim(a.c.dim) * 4, 256) + align_up(part_rows_of(a) * 8, 256);
-        if (with_mass) b += align_up((uint64_t)a.n_rows * a.c.n_kv * a.group * a.tokens * a.score_len * 4, 256);
-    }
+    if (a.slot_goal) b += align_up(part_rows_of(a) * padded_dim(a.c.dim) * 4, 256);
+    if (a.slot_goal || with_mass) b += align_up(part_rows_of(a) * 8, 256) + align_up((uint64_t)a.n_rows * 8, 256);
+    if (with_mass) b += align_up((uint64_t)a.n_rows * a.c.n_kv * a.group * a.tokens * a.score_len * 4, 256);
     return b;
 }
 
-// Of query row r of (row, head): where its partial results begin, and how far
-// apart the splits lie, in query rows.
-__device__ inline uint64_t part_at(const DecodeArgs &a, uint32_t row, uint32_t head, uint32_t r, uint32_t unit_rows,
-                                   uint64_t &stride)
+// Partial result of query row r in slot `slot` of a head, in rows; the slots
+// of a row lie n_kv * n_tiles * part_rows apart.
+__device__ __forceinline__ uint64_t part_at(const DecodeArgs &a, uint32_t slot, uint32_t head, uint32_t r, uint32_t unit_rows)
 {
-    const uint64_t unit = ((uint64_t)row * a.c.n_kv + head) * a.n_tiles + r / unit_rows;
-    stride = a.part_rows;
-    return unit * a.n_splits * a.part_rows + r % unit_rows;
+    return (((uint64_t)slot * a.c.n_kv + head) * a.n_tiles + r / unit_rows) * a.part_rows + r % unit_rows;
 }
 
-__device__ inline uint32_t length_of(const DecodeArgs &a, uint32_t row, uint32_t &req)
+// Maximum and sum over the slots of one query row, by kLanes adjacent lanes.
+template <int kLanes>
+__device__ inline floatx2 join_ml(const float *ml, uint64_t stride, uint32_t slots)
 {
-    req = a.rows ? a.rows[row] : row;
-    const uint32_t n = req < a.c.n_requests ? a.c.len[req] : 0;
-    return n < a.c.cap ? n : a.c.cap;
-}
-
-// Maximum and sum over the splits of one query row, by one wave.
-__device__ inline floatx2 join_ml(const DecodeArgs &a, uint64_t at, uint64_t stride, uint32_t splits)
-{
-    float top = -__builtin_inff(), l = 0.0f;
-    for (uint32_t s = lane_id(); s < splits; s += 64) top = fmaxf(top, a.part_ml[2 * (at + s * stride)]);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    for (uint32_t s = lane_id(); s < splits; s += 64) {
-        const floatx2 x = *reinterpret_cast<const floatx2 *>(a.part_ml + 2 * (at + s * stride));
-        l += x[1] * __builtin_amdgcn_exp2f(x[0] - finite_or_zero(top));
+    const uint32_t t = threadIdx.x % kLanes;
+    floatx2 x = {-__builtin_inff(), 0.0f};
+    for (uint32_t s = t; s < slots; s += kLanes) {
+        const floatx2 y = *reinterpret_cast<const floatx2 *>(ml + 2 * s * stride);
+        const float top = finite_or_zero(fmaxf(x[0], y[0]));
+        x = floatx2{fmaxf(x[0], y[0]), x[1] * __builtin_amdgcn_exp2f(x[0] - top) + y[1] * __builtin_amdgcn_exp2f(y[0] - top)};
     }
+    float top = x[0];
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    for (int d = kLanes / 2; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    float l = x[1] * __builtin_amdgcn_exp2f(x[0] - finite_or_zero(top));
+#pragma unroll
+    for (int d = kLanes / 2; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
     return floatx2{top, l};
 }
 
-// The first join_groups workgroups join the splits of four query rows each;
-// the others sum the weights of kMassTokens tokens of one (row, head).
+// The first n_rows * n_kv * query rows workgroups (none where no row is cut)
+// join the slots of one query row each; the others sum the weights of
+// kMassTokens tokens. Both are chains of a few loads from what other dies
+// wrote, a microsecond each, so each chain is kept short and there are many.
 template <typename T, int kDim>
 __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t join_groups, uint32_t mass_groups,
                                                    uint32_t unit_rows)
 {
-    constexpr int kPer = kDim / 64;
+    constexpr int kLanes = kDim / 4;                  // lanes of one partial row
+    constexpr int kTeams = 256 / kLanes;
     const KvView &c = a.c;
     const uint32_t query_rows = a.group * a.tokens;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const uint64_t stride = (uint64_t)c.n_kv * a.n_tiles * a.part_rows;
     if (blockIdx.x < join_groups) {
-        const uint64_t id = (uint64_t)blockIdx.x * 4 + wave;
-        if (id >= (uint64_t)a.n_rows * c.n_kv * query_rows) return;
-        const uint32_t r = (uint32_t)(id % query_rows), head = (uint32_t)(id / query_rows % c.n_kv);
-        const uint32_t row = (uint32_t)(id / query_rows / c.n_kv);
-        uint32_t req;
-        const uint32_t n = length_of(a, row, req);
-        const Span span = span_of(n, a.tokens, a.window, a.sinks);
-        const uint32_t splits = span.total ? (span.total + a.split_blocks - 1) / a.split_blocks : 1;
-        uint64_t stride;
-        const uint64_t at = part_at(a, row, head, r, unit_rows, stride);
-        const floatx2 ml = join_ml(a, at, stride, splits);
-        float o[kPer];
-#pragma unroll
-        for (int k = 0; k < kPer; k++) o[k] = 0.0f;
-        const float *from = a.part_o + at * kDim + lane_id() * kPer;
+        __shared__ __align__(16) float sm_o[kTeams][kDim];
+        const uint32_t r = blockIdx.x % query_rows, head = blockIdx.x / query_rows % c.n_kv;
+        const uint32_t row = blockIdx.x / query_rows / c.n_kv;
+        const uint32_t first = a.row_slots[2 * row], count = a.row_slots[2 * row + 1];
+        if (count == 1) return;
+        const uint64_t at = part_at(a, first, head, r, unit_rows);
+        const uint32_t team = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+        const float *from = a.part_o + at * kDim + d, *m = a.part_ml + 2 * at;
+        const floatx2 ml = join_ml<kLanes>(m, stride, count);
         const float base = finite_or_zero(ml[0]);
+        floatx4 o = {0, 0, 0, 0};
 #pragma unroll 8
-        for (uint32_t s = 0; s < splits; s++) {
-            const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * (at + s * stride)] - base);
+        for (uint32_t s = team; s < count; s += kTeams) {
+            const float f = __builtin_amdgcn_exp2f(m[2 * s * stride] - base);
+            const floatx4 x = *reinterpret_cast<const floatx4 *>(from + s * stride * kDim);
 #pragma unroll
-            for (int k = 0; k < kPer; k++) o[k] += f * from[s * stride * kDim + k];
+            for (int e = 0; e < 4; e++) o[e] += f * x[e];
         }
-        const float inv = ml[1] == 0.0f ? 0.0f : (c.type == DS_E4M3 && c.v_scale ? c.v_scale[head] : 1.0f) / ml[1];
-        const uint32_t tok = r / a.group, h = r % a.group;
-        uint16_t *to = static_cast<uint16_t *>(a.out) +
-                       (((uint64_t)row * a.tokens + tok) * c.n_kv * a.group + (uint64_t)head * a.group + h) * c.dim;
+        *reinterpret_cast<floatx4 *>(&sm_o[team][d]) = o;
+        __syncthreads();
+        if (team == 0 && d < c.dim) {
+            for (int k = 1; k < kTeams; k++) {
+                const floatx4 x = *reinterpret_cast<const floatx4 *>(&sm_o[k][d]);
 #pragma unroll
-        for (int k = 0; k < kPer; k++) {
-            const uint32_t d = lane_id() * kPer + k;
-            if (d < c.dim) to[d] = (uint16_t)T::pack(o[k] * inv, 0.0f);
+                for (int e = 0; e < 4; e++) o[e] += x[e];
+            }
+            const float inv = ml[1] == 0.0f ? 0.0f : (c.type == DS_E4M3 && c.v_scale ? c.v_scale[head] : 1.0f) / ml[1];
+            const uint32_t tok = r / a.group, h = r % a.group;
+            uint16_t *to = static_cast<uint16_t *>(a.out) +
+                           (((uint64_t)row * a.tokens + tok) * c.n_kv * a.group + (uint64_t)head * a.group + h) * c.dim + d;
+            *reinterpret_cast<uintx2 *>(to) = uintx2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
         }
         return;
     }
@@ -128,12 +124,10 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t 
     const uint32_t n = length_of(a, row, req);
     const Span span = span_of(n, a.tokens, a.window, a.sinks);
     if (chunk * (kMassTokens / kBlockTokens) >= span.total) return;
-    const uint32_t splits = (span.total + a.split_blocks - 1) / a.split_blocks;
-    for (uint32_t r = wave; r < query_rows; r += 4) {
-        uint64_t stride;
-        const uint64_t at = part_at(a, row, head, r, unit_rows, stride);
-        const floatx2 ml = join_ml(a, at, stride, splits);
-        if (lane_id() == 0) {
+    const uint32_t first = a.row_slots[2 * row], count = a.row_slots[2 * row + 1];
+    for (uint32_t r = threadIdx.x / 16; r < query_rows; r += 16) {
+        const floatx2 ml = join_ml<16>(a.part_ml + 2 * part_at(a, first, head, r, unit_rows), stride, count);
+        if (threadIdx.x % 16 == 0) {
             sm_m[r] = finite_or_zero(ml[0]);
             sm_inv[r] = ml[1] == 0.0f ? 0.0f : 1.0f / ml[1];
         }
@@ -145,6 +139,7 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t 
     const uint32_t j = b * kBlockTokens + tok % kBlockTokens;
     const float *from = a.scores + ((uint64_t)row * c.n_kv + head) * query_rows * a.score_len + tok;
     floatx4 w = {0, 0, 0, 0};
+#pragma unroll 4
     for (uint32_t r = 0; r < query_rows; r++) {
         const floatx4 s = *reinterpret_cast<const floatx4 *>(from + (uint64_t)r * a.score_len);
 #pragma unroll
@@ -160,7 +155,7 @@ template <typename T>
 static hipError_t join(const DecodeArgs &a, hipStream_t s)
 {
     const uint32_t query_rows = a.group * a.tokens, unit_rows = 16 * unit_tiles(a.c.dim, query_rows);
-    const uint32_t groups = (uint32_t)cdiv((uint64_t)a.n_rows * a.c.n_kv * query_rows, 4);
+    const uint32_t groups = a.slot_goal ? a.n_rows * a.c.n_kv * query_rows : 0;
     const uint32_t mass_groups = a.mass ? (uint32_t)cdiv(a.score_len, kMassTokens) : 0;
     const uint32_t grid = groups + a.n_rows * a.c.n_kv * mass_groups;
     const uint32_t dim = padded_dim(a.c.dim);
@@ -176,18 +171,23 @@ static hipError_t join(const DecodeArgs &a, hipStream_t s)
 hipError_t decode_launch(DecodeArgs a, void *ws, hipStream_t s)
 {
     a.part_o = a.part_ml = a.scores = nullptr;
-    if (a.n_splits > 1 || a.mass) {
-        uint8_t *p = static_cast<uint8_t *>(ws);
+    a.row_slots = nullptr;
+    uint8_t *p = static_cast<uint8_t *>(ws);
+    if (a.slot_goal) {
         a.part_o = reinterpret_cast<float *>(p);
         p += align_up(part_rows_of(a) * padded_dim(a.c.dim) * 4, 256);
+    }
+    if (a.slot_goal || a.mass) {
         a.part_ml = reinterpret_cast<float *>(p);
         p += align_up(part_rows_of(a) * 8, 256);
-        if (a.mass) a.scores = reinterpret_cast<float *>(p);
+        a.row_slots = reinterpret_cast<uint32_t *>(p);
+        p += align_up((uint64_t)a.n_rows * 8, 256);
     }
+    if (a.mass) a.scores = reinterpret_cast<float *>(p);
     const bool bf16 = a.q_type == DS_BF16, e4m3 = a.c.type == DS_E4M3;
     hipError_t e = e4m3 ? (bf16 ? decode_attend_bf16_e4m3(a, s) : decode_attend_f16_e4m3(a, s))
                         : (bf16 ? decode_attend_bf16(a, s) : decode_attend_f16(a, s));
-    if (e != hipSuccess || !a.part_o) return e;
+    if (e != hipSuccess || !a.part_ml) return e;
     return bf16 ? join<Bf16>(a, s) : join<F16>(a, s);
 }
 

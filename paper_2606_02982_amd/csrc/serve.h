@@ -31,15 +31,17 @@ struct DecodeArgs {
     uint32_t n_rows, group, tokens, window, sinks;
     float scale2;          // scale * log2(e)
     int q_type;
-    // the split: a unit is one row, key-value head and tile of at most 16 or
-    // 32 of the group's query rows
-    uint32_t n_tiles;      // tiles per row and head
-    uint32_t split_blocks; // blocks of 32 tokens per split
-    uint32_t n_splits;     // splits of the longest row
+    // The split. A slot is a run of blocks of one row; it has n_kv pairs
+    // (slot, head), and a pair one unit per tile of 16 or 32 query rows. Which
+    // blocks a slot holds follows on the device from the batch's lengths.
+    uint32_t n_tiles;      // tiles per pair
+    uint32_t n_slots;      // most slots of a batch of this size
+    uint32_t slot_goal;    // slots wanted where the caches are long enough; 0: one per row
     uint32_t part_rows;    // query rows of a unit's partial result
     uint32_t score_len;    // tokens of a row of scores
-    float *part_o;         // (unit, split, part_rows, padded dim)
-    float *part_ml;        // (unit, split, part_rows, 2): running maximum and sum
+    float *part_o;         // (unit, part_rows, padded dim); a row in one slot has none
+    float *part_ml;        // (unit, part_rows, 2): running maximum and sum
+    uint32_t *row_slots;   // (row, 2): its first slot and their number
     float *scores;         // (row, head, query row, score_len), for mass
 };
 
