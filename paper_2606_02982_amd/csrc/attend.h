@@ -78,11 +78,21 @@ struct F16 {
     }
 };
 
+// The largest of x over lanes m, m + 16, m + 32, m + 48.
+__device__ __forceinline__ float max_over_groups(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+    const uint32_t w = __builtin_bit_cast(uint32_t, x);
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builtin_inff() ? 0.0f : m; }
 
 typedef const __attribute__((address_space(4))) uint32_t *ScalarU32;   // read-only during the launch: scalar loads
 
-constexpr uint32_t kMinSlotBlocks = 8;     // two blocks per wave
 constexpr uint32_t kBalancedRows = 1024;   // rows whose lengths every workgroup looks through
 
 __device__ __forceinline__ uint32_t length_of(const DecodeArgs &a, uint32_t row, uint32_t &req)
@@ -101,7 +111,7 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 // The row that slot `want` belongs to. Rows differ in length, so slots are
 // cut from the batch's blocks as a whole: of all rows' blocks a slot gets at
-// most ceil(blocks / slot_goal), at least kMinSlotBlocks, and a row is cut
+// most ceil(blocks / slot_goal), at least slot_blocks, and a row is cut
 // into equal slots of at most that. Every workgroup of 256 threads finds this
 // by itself, looking through the rows' lengths (a launch before would cost
 // more than the few hundred cycles).
@@ -136,7 +146,7 @@ __device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
     all = sm_blocks[0] + sm_blocks[1] + sm_blocks[2] + sm_blocks[3];
     // all < 2^37: a float holds the quotient to far less than a slot
     uint32_t most = (uint32_t)((float)all / (float)a.slot_goal) + 1;
-    most = most > kMinSlotBlocks ? most : kMinSlotBlocks;
+    most = most > a.slot_blocks ? most : a.slot_blocks;
     auto slots_of = [&](uint32_t t) { return t <= most ? 1u : (t + most - 1) / most; };
     uint32_t own = 0;
     for (uint32_t r = r0; r < r1; r++) {
@@ -166,13 +176,20 @@ __device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
     return Slots{same(0), same(1), same(2), same(3), same(4)};
 }
 
-// One wave's share of a unit: blocks v0 + wave, v0 + wave + 4, ... of the slot
+// One wave's share of a unit: steps wave, wave + 4, ... of the slot's blocks
 // (see DecodeArgs for slots and units).
 // kDim: padded dimensions; kTiles: 16-row tiles of queries; kFast: all kDim
 // dimensions are there and a page holds a multiple of 16 tokens, so half a
 // block lies in one page, its address is the same for the whole wave, and a
 // lane's place in it is a 32-bit offset. Otherwise addresses are per lane.
-template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast>
+// A step takes as many blocks as make 16 KB of keys and values (8 KB for 64
+// dimensions in 8 bits), the same registers whatever the type: the chain of a
+// step (products, maximum over the lanes, exponentials, products) is as long
+// for few bytes as for many.
+template <int kDim, int kElem, int kTiles>
+constexpr int kSubBlocks = kDim * kElem >= 256 || kTiles > 1 ? 1 : 2;
+
+template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast, bool kStream>
 struct Attender {
     static constexpr int kElem = kE4m3 ? 1 : 2;
     static constexpr int kStepsK = kDim / 32;                  // matrix steps per score
@@ -181,6 +198,7 @@ struct Attender {
     static constexpr int kVd = kDim / 16 / kParts;             // V: dimensions per lane and piece
     static constexpr int kVw = kVd * kElem / 4;                // V: 32-bit words per lane, token and piece
     static constexpr int kOut = kDim / 16;                     // 16-dimension tiles of O^T
+    static constexpr int kSub = kSubBlocks<kDim, kElem, kTiles>;       // blocks of 32 tokens per step
 
     // Where a block's tokens are.
     struct Place {
@@ -203,8 +221,9 @@ struct Attender {
     int pos[kTiles];
     float mx[kTiles], sum[kTiles];
     floatx4 acc[kTiles][kOut];
-    uintx4 kr[2][kLoadsK];
-    uint32_t vr[8][kParts][kVw];
+    uintx4 kr[kSub][2][kLoadsK];
+    uint32_t vr[kSub][8][kParts][kVw];
+    uint32_t page[kSub][2];                                    // kFast: of the step after next
 
     __device__ __forceinline__ uint32_t block_of(uint32_t v) const
     {
@@ -215,16 +234,19 @@ struct Attender {
         return a.c.page_shift >= 0 ? j >> a.c.page_shift : j / a.c.page_size;
     }
 
-    // The pages of block v's halves (kFast; no page where there is no token).
-    __device__ __forceinline__ void pages(uint32_t v, uint32_t v1, uint32_t *page) const
+    // The pages of the halves of blocks v, v + 1, .. (kFast; no page where there is no token).
+    __device__ __forceinline__ void pages(uint32_t v, uint32_t v1)
     {
-        const uint32_t j0 = block_of(v) * kBlockTokens;
 #pragma unroll
-        for (int i = 0; i < 2; i++)
-            page[i] = v < v1 && j0 + 16 * i < n ? table[page_of(j0 + 16 * i)] : 0xFFFFFFFFu;
+        for (int b = 0; b < kSub; b++) {
+            const uint32_t j0 = block_of(v + b) * kBlockTokens;
+#pragma unroll
+            for (int i = 0; i < 2; i++)
+                page[b][i] = v + b < v1 && j0 + 16 * i < n ? table[page_of(j0 + 16 * i)] : 0xFFFFFFFFu;
+        }
     }
 
-    __device__ __forceinline__ Place place(uint32_t v, const uint32_t *page) const
+    __device__ __forceinline__ Place place(uint32_t v, uint32_t v1, const uint32_t *page) const
     {
         Place p;
         p.j0 = (int)(block_of(v) * kBlockTokens);
@@ -239,12 +261,12 @@ struct Attender {
             }
         } else {
             const uint32_t j = (uint32_t)p.j0 + (lane_id() & 31);
-            const uint32_t pg = j < n ? ((const uint32_t *)a.c.table)[(uint64_t)req * a.c.max_pages + page_of(j)] : 0xFFFFFFFFu;
+            const uint32_t pg = v < v1 && j < n ? ((const uint32_t *)a.c.table)[(uint64_t)req * a.c.max_pages + page_of(j)] : 0xFFFFFFFFu;
             const bool ok = pg < a.c.n_pages;
             p.seen = (uint32_t)__ballot(ok);
             p.at = (ok ? pg : 0u) * a.c.page_stride + (j - page_of(j) * a.c.page_size) * a.c.token_stride;
         }
-        const int left = (int)n - p.j0;
+        const int left = v < v1 ? (int)n - p.j0 : 0;
         if (left < 32) p.seen &= (1u << left) - 1u;
         return p;
     }
@@ -254,20 +276,33 @@ struct Attender {
                (uint32_t)__shfl((int)(uint32_t)p.at, token, 64);
     }
 
-    __device__ __forceinline__ void load_k(const Place &p)
+    // kStream: whole cache lines that no other workgroup reads go past the
+    // caches (16 heads of 128 dimensions in 16 bits: 380 -> 370 us for 2.1 GB,
+    // 8 heads of 256: 348 -> 336 us; in 8 bits 217 -> 222 us, two tiles of
+    // query rows 268 -> 365 us).
+    template <typename W>
+    static __device__ __forceinline__ W fetch(const uint8_t *p)
+    {
+        if constexpr (kStream)
+            return __builtin_nontemporal_load(reinterpret_cast<const W *>(p));
+        else
+            return *reinterpret_cast<const W *>(p);
+    }
+
+    __device__ __forceinline__ void load_k(const Place &p, uintx4 (&kr)[2][kLoadsK])
     {
 #pragma unroll
         for (int i = 0; i < 2; i++) {
             if constexpr (kFast) {
                 const uint8_t *base = kh + p.base[i] * kElem;
 #pragma unroll
-                for (int s = 0; s < kLoadsK; s++) kr[i][s] = *reinterpret_cast<const uintx4 *>(base + k_lane + s * 64);
+                for (int s = 0; s < kLoadsK; s++) kr[i][s] = fetch<uintx4>(base + k_lane + s * 64);
             } else {
                 const uint8_t *base = kh + at_of(p, 16 * i + m) * kElem;
 #pragma unroll
                 for (int s = 0; s < kLoadsK; s++) {
                     const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
-                    kr[i][s] = *reinterpret_cast<const uintx4 *>(base + (d < a.c.dim ? d : 0) * kElem);
+                    kr[i][s] = fetch<uintx4>(base + (d < a.c.dim ? d : 0) * kElem);
                 }
 #pragma unroll
                 for (int s = 0; s < kLoadsK; s++) {
@@ -279,7 +314,7 @@ struct Attender {
     }
 
     // dimensions kVd m .. of each piece, for the lane's eight tokens, as stored
-    __device__ __forceinline__ void load_v(const Place &p)
+    __device__ __forceinline__ void load_v(const Place &p, uint32_t (&vr)[8][kParts][kVw])
     {
 #pragma unroll
         for (int j = 0; j < 8; j++) {
@@ -293,15 +328,15 @@ struct Attender {
                 const uint32_t d = h * 128 + m * kVd;
                 const uint8_t *src = kFast ? base + h * 128 * kElem : base + (d < a.c.dim ? d : 0) * kElem;
                 if constexpr (kVw == 4) {
-                    const uintx4 x = *reinterpret_cast<const uintx4 *>(src);
+                    const uintx4 x = fetch<uintx4>(src);
 #pragma unroll
                     for (int w = 0; w < 4; w++) vr[j][h][w] = x[w];
                 } else if constexpr (kVw == 2) {
-                    const uintx2 x = *reinterpret_cast<const uintx2 *>(src);
+                    const uintx2 x = fetch<uintx2>(src);
                     vr[j][h][0] = x[0];
                     vr[j][h][1] = x[1];
                 } else {
-                    vr[j][h][0] = *reinterpret_cast<const uint32_t *>(src);
+                    vr[j][h][0] = fetch<uint32_t>(src);
                 }
             }
         }
@@ -333,16 +368,20 @@ struct Attender {
             for (int x = 0; x < kOut; x++) acc[t][x] = floatx4{0, 0, 0, 0};
         }
         if (v >= v1) return;
-        uint32_t page[2];
-        if (kFast) pages(v, v1, page);
-        Place here = place(v, page);
-        load_k(here);
-        load_v(here);
-        if (kFast) pages(v + 4, v1, page);
-        for (;;) {
-            floatx4 s[kTiles][2];
+        if (kFast) pages(v, v1);
+        Place here[kSub];
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+        for (int b = 0; b < kSub; b++) {
+            here[b] = place(v + b, v1, page[b]);
+            load_k(here[b], kr[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < kSub; b++) load_v(here[b], vr[b]);
+        if (kFast) pages(v + 4 * kSub, v1);
+        for (;;) {
+            floatx4 s[kTiles][2 * kSub];
+#pragma unroll
+            for (int i = 0; i < 2 * kSub; i++)
 #pragma unroll
                 for (int t = 0; t < kTiles; t++) {
                     s[t][i] = floatx4{0, 0, 0, 0};
@@ -350,52 +389,60 @@ struct Attender {
                     for (int st = 0; st < kStepsK; st++) {
                         uintx4 kf;
                         if constexpr (kE4m3) {
-                            const uint32_t w0 = kr[i][st >> 1][(st & 1) * 2], w1 = kr[i][st >> 1][(st & 1) * 2 + 1];
+                            const uint32_t w0 = kr[i >> 1][i & 1][st >> 1][(st & 1) * 2], w1 = kr[i >> 1][i & 1][st >> 1][(st & 1) * 2 + 1];
                             kf = uintx4{T::template from_e4m3<false>(w0), T::template from_e4m3<true>(w0),
                                         T::template from_e4m3<false>(w1), T::template from_e4m3<true>(w1)};
                         } else {
-                            kf = kr[i][st];
+                            kf = kr[i >> 1][i & 1][st];
                         }
                         s[t][i] = T::mfma(kf, q[t][st], s[t][i]);
                     }
                 }
-            const bool more = v + 4 < v1;
-            Place next = here;
+            const bool more = v + 4 * kSub < v1;
+            Place next[kSub];
             if (more) {
-                next = place(v + 4, page);
-                load_k(next);
-                if (kFast) pages(v + 8, v1, page);
+#pragma unroll
+                for (int b = 0; b < kSub; b++) {
+                    next[b] = place(v + 4 * kSub + b, v1, page[b]);
+                    load_k(next[b], kr[b]);
+                }
+                if (kFast) pages(v + 8 * kSub, v1);
             }
 
             // which tokens any query sees; whether every query sees all
-            uint32_t seen = here.seen;
-            const int j0 = here.j0;
-            const bool full = seen == 0xFFFFFFFFu && j0 + 31 <= first_pos &&
-                              (a.window == 0 || j0 > (int)n - 1 - (int)a.window || j0 + 31 < (int)a.sinks);
-            if (!full) {
-                uint32_t near = 0xFFFFFFFFu;            // at or behind the window's start
-                if (lo > j0) near = lo - j0 < 32 ? ~((1u << (lo - j0)) - 1u) : 0u;
-                uint32_t sink = 0;
-                if ((int)a.sinks > j0) sink = (int)a.sinks - j0 < 32 ? (1u << ((int)a.sinks - j0)) - 1u : 0xFFFFFFFFu;
-                seen &= near | sink;
+            uint32_t seen[kSub];
+            bool full[kSub];
 #pragma unroll
-                for (int t = 0; t < kTiles; t++)
+            for (int b = 0; b < kSub; b++) {
+                const int j0 = here[b].j0;
+                seen[b] = here[b].seen;
+                full[b] = seen[b] == 0xFFFFFFFFu && j0 + 31 <= first_pos &&
+                          (a.window == 0 || j0 > (int)n - 1 - (int)a.window || j0 + 31 < (int)a.sinks);
+                if (!full[b]) {
+                    uint32_t near = 0xFFFFFFFFu;        // at or behind the window's start
+                    if (lo > j0) near = lo - j0 < 32 ? ~((1u << (lo - j0)) - 1u) : 0u;
+                    uint32_t sink = 0;
+                    if ((int)a.sinks > j0) sink = (int)a.sinks - j0 < 32 ? (1u << ((int)a.sinks - j0)) - 1u : 0xFFFFFFFFu;
+                    seen[b] &= near | sink;
 #pragma unroll
-                    for (int i = 0; i < 2; i++)
+                    for (int t = 0; t < kTiles; t++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const int bit = 16 * i + g * 4 + e, j = j0 + bit;
-                            const bool on = ((seen >> bit) & 1u) && j <= pos[t] &&
-                                            (a.window == 0 || j > pos[t] - (int)a.window || j < (int)a.sinks);
-                            s[t][i][e] = on ? s[t][i][e] * scale : -__builtin_inff();
-                        }
-            } else {
+                        for (int i = 0; i < 2; i++)
 #pragma unroll
-                for (int t = 0; t < kTiles; t++)
+                            for (int e = 0; e < 4; e++) {
+                                const int bit = 16 * i + g * 4 + e, j = j0 + bit;
+                                const bool on = ((seen[b] >> bit) & 1u) && j <= pos[t] &&
+                                                (a.window == 0 || j > pos[t] - (int)a.window || j < (int)a.sinks);
+                                s[t][2 * b + i][e] = on ? s[t][2 * b + i][e] * scale : -__builtin_inff();
+                            }
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 2; i++)
+                    for (int t = 0; t < kTiles; t++)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) s[t][i][e] *= scale;
+                        for (int i = 0; i < 2; i++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) s[t][2 * b + i][e] *= scale;
+                }
             }
             if (a.scores) {
 #pragma unroll
@@ -405,21 +452,21 @@ struct Attender {
                         float *to = a.scores + (((uint64_t)row * a.c.n_kv + head) * query_rows + r) * a.score_len +
                                     (uint64_t)v * kBlockTokens + g * 4;
 #pragma unroll
-                        for (int i = 0; i < 2; i++) *reinterpret_cast<floatx4 *>(to + 16 * i) = s[t][i];
+                        for (int i = 0; i < 2 * kSub; i++)
+                            if (v + i / 2 < v1) *reinterpret_cast<floatx4 *>(to + 16 * i) = s[t][i];
                     }
                 }
             }
             // softmax step: s becomes the weights
-            uintx4 p_hi[kTiles], p_lo[kTiles];
+            uintx4 p_hi[kTiles][kSub], p_lo[kTiles][kSub];
 #pragma unroll
             for (int t = 0; t < kTiles; t++) {
                 float top = -__builtin_inff();
 #pragma unroll
-                for (int i = 0; i < 2; i++)
+                for (int i = 0; i < 2 * kSub; i++)
 #pragma unroll
                     for (int e = 0; e < 4; e++) top = fmaxf(top, s[t][i][e]);
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                top = max_over_groups(top);
                 if (__any(top > mx[t])) {
                     const float grown = fmaxf(mx[t], top);
                     const float f = __builtin_amdgcn_exp2f(mx[t] - finite_or_zero(grown));
@@ -432,106 +479,119 @@ struct Attender {
                 }
                 const float base = finite_or_zero(mx[t]);
 #pragma unroll
-                for (int i = 0; i < 2; i++)
+                for (int i = 0; i < 2 * kSub; i++)
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         s[t][i][e] = __builtin_amdgcn_exp2f(s[t][i][e] - base);
                         sum[t] += s[t][i][e];
                     }
 #pragma unroll
-                for (int i = 0; i < 2; i++)
+                for (int i = 0; i < 2 * kSub; i++)
 #pragma unroll
                     for (int e = 0; e < 4; e += 2) {
                         const uint32_t w = T::pack(s[t][i][e], s[t][i][e + 1]);
-                        p_hi[t][i * 2 + e / 2] = w;
-                        p_lo[t][i * 2 + e / 2] = T::pack(s[t][i][e] - T::lo(w), s[t][i][e + 1] - T::hi(w));
+                        p_hi[t][i >> 1][(i & 1) * 2 + e / 2] = w;
+                        p_lo[t][i >> 1][(i & 1) * 2 + e / 2] = T::pack(s[t][i][e] - T::lo(w), s[t][i][e + 1] - T::hi(w));
                     }
             }
-            if (!full) {
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const bool on = (seen >> ((j >> 2) * 16 + g * 4 + (j & 3))) & 1u;
-#pragma unroll
-                    for (int h = 0; h < kParts; h++)
-#pragma unroll
-                        for (int w = 0; w < kVw; w++) vr[j][h][w] = on ? vr[j][h][w] : 0u;
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < kParts; h++)
-#pragma unroll
-                for (int d = 0; d < kVd; d += 2) {
-                    uint32_t pair[8];                   // dimensions d, d + 1 of the eight tokens
+            for (int b = 0; b < kSub; b++) {
+                if (!full[b]) {
 #pragma unroll
                     for (int j = 0; j < 8; j++) {
-                        if constexpr (kE4m3)
-                            pair[j] = (d & 2) ? T::template from_e4m3<true>(vr[j][h][d >> 2])
-                                              : T::template from_e4m3<false>(vr[j][h][d >> 2]);
-                        else
-                            pair[j] = vr[j][h][d >> 1];
-                    }
+                        const bool on = (seen[b] >> ((j >> 2) * 16 + g * 4 + (j & 3))) & 1u;
 #pragma unroll
-                    for (int o = 0; o < 2; o++) {
-                        const int x = h * kVd + d + o;
-                        const uint32_t sel = o ? 0x07060302u : 0x05040100u;
-                        uintx4 vf;
+                        for (int h = 0; h < kParts; h++)
 #pragma unroll
-                        for (int w = 0; w < 4; w++) vf[w] = __builtin_amdgcn_perm(pair[2 * w + 1], pair[2 * w], sel);
-                        if constexpr (!kCareful) {
-#pragma unroll
-                            for (int t = 0; t < kTiles; t++) {
-                                acc[t][x] = T::mfma(vf, p_hi[t], acc[t][x]);
-                                acc[t][x] = T::mfma(vf, p_lo[t], acc[t][x]);
-                            }
-                        } else {
-                            // lane (m, g) adds dimensions 4 g + i of column m
-#pragma unroll 1
-                            for (int from = 0; from < 4; from++)
-#pragma unroll
-                                for (int j = 0; j < 8; j++)
-#pragma unroll
-                                    for (int t = 0; t < kTiles; t++) {
-                                        const float pw = __shfl(s[t][j >> 2][j & 3], from * 16 + m, 64);
-#pragma unroll
-                                        for (int i = 0; i < 4; i++) {
-                                            const uint32_t w = (uint32_t)__shfl((int)vf[j >> 1], from * 16 + g * 4 + i, 64);
-                                            const float val = (j & 1) ? T::hi(w) : T::lo(w);
-                                            if (pw != 0.0f) acc[t][x][i] += pw * val;
-                                        }
-                                    }
-                        }
+                            for (int w = 0; w < kVw; w++) vr[b][j][h][w] = on ? vr[b][j][h][w] : 0u;
                     }
                 }
+#pragma unroll
+                for (int h = 0; h < kParts; h++)
+#pragma unroll
+                    for (int d = 0; d < kVd; d += 2) {
+                        uint32_t pair[8];               // dimensions d, d + 1 of the eight tokens
+#pragma unroll
+                        for (int j = 0; j < 8; j++) {
+                            if constexpr (kE4m3)
+                                pair[j] = (d & 2) ? T::template from_e4m3<true>(vr[b][j][h][d >> 2])
+                                                  : T::template from_e4m3<false>(vr[b][j][h][d >> 2]);
+                            else
+                                pair[j] = vr[b][j][h][d >> 1];
+                        }
+#pragma unroll
+                        for (int o = 0; o < 2; o++) {
+                            const int x = h * kVd + d + o;
+                            const uint32_t sel = o ? 0x07060302u : 0x05040100u;
+                            uintx4 vf;
+#pragma unroll
+                            for (int w = 0; w < 4; w++) vf[w] = __builtin_amdgcn_perm(pair[2 * w + 1], pair[2 * w], sel);
+                            if constexpr (!kCareful) {
+#pragma unroll
+                                for (int t = 0; t < kTiles; t++) {
+                                    acc[t][x] = T::mfma(vf, p_hi[t][b], acc[t][x]);
+                                    acc[t][x] = T::mfma(vf, p_lo[t][b], acc[t][x]);
+                                }
+                            } else {
+                                // lane (m, g) adds dimensions 4 g + i of column m
+#pragma unroll 1
+                                for (int from = 0; from < 4; from++)
+#pragma unroll
+                                    for (int j = 0; j < 8; j++)
+#pragma unroll
+                                        for (int t = 0; t < kTiles; t++) {
+                                            const float pw = __shfl(s[t][2 * b + (j >> 2)][j & 3], from * 16 + m, 64);
+#pragma unroll
+                                            for (int i = 0; i < 4; i++) {
+                                                const uint32_t w = (uint32_t)__shfl((int)vf[j >> 1], from * 16 + g * 4 + i, 64);
+                                                const float val = (j & 1) ? T::hi(w) : T::lo(w);
+                                                if (pw != 0.0f) acc[t][x][i] += pw * val;
+                                            }
+                                        }
+                            }
+                        }
+                    }
+            }
             if (!more) break;
-            here = next;
-            load_v(here);
-            v += 4;
+#pragma unroll
+            for (int b = 0; b < kSub; b++) {
+                here[b] = next[b];
+                load_v(here[b], vr[b]);
+            }
+            v += 4 * kSub;
         }
     }
     uint32_t req;
 };
 
-template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast>
-__global__ __launch_bounds__(256, (kDim * kTiles <= 64    ? (kFast ? 4 : 3)
-                                   : kDim * kTiles <= 128 ? (kFast ? 3 : 2)
-                                   : kDim <= 128          ? (kFast ? 2 : 1)
-                                                          : 1))
+// Waves per SIMD that the registers are limited to: as many as fit without spills.
+template <int kWidth, int kSub, bool kFast>
+constexpr int kWaves = kWidth <= 64 ? (kSub == 1 || kFast ? 3 : 2) : kWidth <= 128 ? (kSub == 1 && kFast ? 3 : 2) : kWidth <= 256 && kFast ? 2 : 1;
+
+template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast, bool kStream>
+__global__ __launch_bounds__(256, (kWaves<kDim == 256 ? 512 : kDim * kTiles, kSubBlocks<kDim, kE4m3 ? 1 : 2, kTiles>, kFast>))
 void attend_kernel(const DecodeArgs a)
 {
-    typedef Attender<T, kE4m3, kDim, kTiles, kFast> A;
+    typedef Attender<T, kE4m3, kDim, kTiles, kFast, kStream> A;
     constexpr int kRows = 16 * kTiles;
     constexpr int kPitch = kDim + 4;
 
     __shared__ float sm_m[4][kRows], sm_l[4][kRows];
-    __shared__ __align__(16) float sm_o[kRows * kPitch];
+    __shared__ __align__(16) float sm_o[4][kRows * kPitch];
 
     const KvView &c = a.c;
     const int lane = lane_id(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    // units of one pair on one of the eight dies (workgroups go round them):
-    // they read the same keys and values
-    const uint32_t round = blockIdx.x / (8 * a.n_tiles), within = blockIdx.x % (8 * a.n_tiles);
-    const uint32_t tile = within / 8, pair = round * 8 + within % 8;
+    // Workgroups go round the eight dies, each with a cache of its own. Units
+    // of one pair, which read the same keys and values, go to one die; so do
+    // all heads of a slot where a token's key is at most 128 bytes, a cache
+    // line (8-bit, 8 heads: 64 dimensions 92 -> 69 us for 268 MB, 128
+    // dimensions 119 -> 116 us for 537 MB; 16-bit, 128 dimensions the other
+    // way round: 198 -> 202 us for 1.07 GB).
+    const uint32_t of_slot = a.by_slot ? c.n_kv : 1;
+    const uint32_t round = blockIdx.x / (8 * a.n_tiles * of_slot), within = blockIdx.x % (8 * a.n_tiles * of_slot);
+    const uint32_t tile = within / 8 % a.n_tiles;
+    const uint32_t pair = (round * 8 + within % 8) * of_slot + within / 8 / a.n_tiles;
     const uint32_t slot = pair / c.n_kv, head = pair % c.n_kv;
     const Slots slots = find_slots(a, slot);
     const uint32_t row = slots.row;
@@ -581,7 +641,7 @@ void attend_kernel(const DecodeArgs a)
         }
     }
 
-    w.template pass<false>(v0 + wave, v1);
+    w.template pass<false>(v0 + wave * A::kSub, v1);
     bool odd = false;
 #pragma unroll
     for (int t = 0; t < kTiles; t++)
@@ -589,12 +649,12 @@ void attend_kernel(const DecodeArgs a)
         for (int x = 0; x < A::kOut; x++)
 #pragma unroll
             for (int e = 0; e < 4; e++) odd = odd || !(fabsf(w.acc[t][x][e]) < __builtin_inff());
-    if (__any(odd)) w.template pass<true>(v0 + wave, v1);
+    if (__any(odd)) w.template pass<true>(v0 + wave * A::kSub, v1);
     auto &mx = w.mx;
     auto &sum = w.sum;
     auto &acc = w.acc;
-    constexpr int kOut = A::kOut, kVd = A::kVd;
-    // join the waves, in their order
+    constexpr int kVd = A::kVd;
+    // the waves' results side by side; they are joined as they are read
 #pragma unroll
     for (int t = 0; t < kTiles; t++) {
         sum[t] += __shfl_xor(sum[t], 16, 64);
@@ -603,42 +663,32 @@ void attend_kernel(const DecodeArgs a)
             sm_m[wave][t * 16 + m] = mx[t];
             sm_l[wave][t * 16 + m] = sum[t];
         }
+#pragma unroll
+        for (int h = 0; h < A::kParts; h++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+#pragma unroll
+                for (int x = h * kVd; x < (h + 1) * kVd; x += 4)
+                    *reinterpret_cast<floatx4 *>(&sm_o[wave][(t * 16 + m) * kPitch + h * 128 + (g * 4 + e) * kVd + x % kVd]) =
+                        floatx4{acc[t][x][e], acc[t][x + 1][e], acc[t][x + 2][e], acc[t][x + 3][e]};
     }
     __syncthreads();
-    float f[kTiles];
-#pragma unroll
-    for (int t = 0; t < kTiles; t++) {
-        float top = sm_m[0][t * 16 + m];
-#pragma unroll
-        for (int k = 1; k < 4; k++) top = fmaxf(top, sm_m[k][t * 16 + m]);
-        f[t] = __builtin_amdgcn_exp2f(mx[t] - finite_or_zero(top));
-    }
-    for (int k = 0; k < 4; k++) {
-        if (wave == k) {
-#pragma unroll
-            for (int t = 0; t < kTiles; t++)
-#pragma unroll
-                for (int x = 0; x < kOut; x++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const int d = (x / kVd) * 128 + (g * 4 + e) * kVd + x % kVd;
-                        float *at = &sm_o[(t * 16 + m) * kPitch + d];
-                        // a wave without tokens has f = 0 and sums of zeros
-                        const float val = acc[t][x][e] * f[t];
-                        *at = k ? *at + val : val;
-                    }
-        }
-        __syncthreads();
-    }
     const uint32_t rows_here = query_rows - tile * kRows < (uint32_t)kRows ? query_rows - tile * kRows : kRows;
     for (uint32_t i = threadIdx.x; i < rows_here * (kDim / 4); i += 256) {
         const uint32_t rr = i / (kDim / 4), d = i % (kDim / 4) * 4;
         float top = sm_m[0][rr], l = 0.0f;
 #pragma unroll
         for (int k = 1; k < 4; k++) top = fmaxf(top, sm_m[k][rr]);
+        floatx4 o = {0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < 4; k++) l += sm_l[k][rr] * __builtin_amdgcn_exp2f(sm_m[k][rr] - finite_or_zero(top));
-        floatx4 o = *reinterpret_cast<const floatx4 *>(&sm_o[rr * kPitch + d]);
+        for (int k = 0; k < 4; k++) {
+            // a wave without tokens has f = 0 and sums of zeros
+            const float f = __builtin_amdgcn_exp2f(sm_m[k][rr] - finite_or_zero(top));
+            l += sm_l[k][rr] * f;
+            const floatx4 x = *reinterpret_cast<const floatx4 *>(&sm_o[k][rr * kPitch + d]);
+#pragma unroll
+            for (int e = 0; e < 4; e++) o[e] += x[e] * f;
+        }
         const uint64_t at = ((uint64_t)pair * a.n_tiles + tile) * a.part_rows + rr;
         if (a.part_ml && d == 0) *reinterpret_cast<floatx2 *>(a.part_ml + 2 * at) = floatx2{top, l};
         if (slots.count > 1) {
@@ -653,15 +703,16 @@ void attend_kernel(const DecodeArgs a)
     }
 }
 
-template <typename T, bool kE4m3, int kDim, int kTiles>
+template <typename T, bool kE4m3, int kDim, int kTiles, bool kStream>
 hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
 {
-    const uint64_t grid = cdiv((uint64_t)a.n_slots * a.c.n_kv, 8) * 8 * a.n_tiles;
+    const uint64_t groups = a.by_slot ? a.n_slots : (uint64_t)a.n_slots * a.c.n_kv;
+    const uint64_t grid = cdiv(groups, 8) * 8 * a.n_tiles * (a.by_slot ? a.c.n_kv : 1);
     // lane offsets in half a block take 32 bits
     if (a.c.page_size % 16 == 0 && a.c.dim == kDim && a.c.token_stride < (1u << 26))
-        attend_kernel<T, kE4m3, kDim, kTiles, true><<<(uint32_t)grid, 256, 0, s>>>(a);
+        attend_kernel<T, kE4m3, kDim, kTiles, true, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
     else
-        attend_kernel<T, kE4m3, kDim, kTiles, false><<<(uint32_t)grid, 256, 0, s>>>(a);
+        attend_kernel<T, kE4m3, kDim, kTiles, false, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -669,9 +720,11 @@ template <typename T, bool kE4m3>
 hipError_t attend(const DecodeArgs &a, hipStream_t s)
 {
     const uint32_t dim = padded_dim(a.c.dim), tiles = unit_tiles(a.c.dim, a.group * a.tokens);
-    if (dim == 64) return tiles == 1 ? attend_page<T, kE4m3, 64, 1>(a, s) : attend_page<T, kE4m3, 64, 2>(a, s);
-    if (dim == 128) return tiles == 1 ? attend_page<T, kE4m3, 128, 1>(a, s) : attend_page<T, kE4m3, 128, 2>(a, s);
-    return attend_page<T, kE4m3, 256, 1>(a, s);
+    if (dim == 64) return tiles == 1 ? attend_page<T, kE4m3, 64, 1, false>(a, s) : attend_page<T, kE4m3, 64, 2, false>(a, s);
+    if (dim == 128) return tiles == 1 ? attend_page<T, kE4m3, 128, 1, !kE4m3>(a, s) : attend_page<T, kE4m3, 128, 2, false>(a, s);
+    if constexpr (!kE4m3)
+        if (a.n_tiles == 1) return attend_page<T, kE4m3, 256, 1, true>(a, s);
+    return attend_page<T, kE4m3, 256, 1, false>(a, s);
 }
 
 }  // namespace ds

@@ -6,7 +6,16 @@
 
 namespace ds {
 
-constexpr uint32_t kPairGoal = 1536;       // pairs of a launch, where the caches are long enough
+// Units of a launch, where the caches are long enough. More of them even out
+// the end of a launch, each costs a start, and a partial result per query
+// row: 32 rows of 8,192 tokens, 8 heads, units 1024 / 1536 / 2048: 256
+// dimensions in 16 bits 348 / 358 / 362 us, 64 dimensions 119 / 113 / 108 us,
+// 128 in 8 bits 118 / 117 / 113 us, 40 query rows 268 / 274 / 276 us; three
+// rows of up to 131,072 tokens, 128 dimensions in 16 bits 264 / 251 / 255 us.
+static uint32_t unit_goal(uint32_t key_bytes, uint32_t unit_tiles)
+{
+    return unit_tiles > 1 || key_bytes > 256 ? 1024 : key_bytes > 128 ? 1536 : 2048;
+}
 constexpr uint32_t kMassTokens = 1024;     // tokens of one workgroup of the weights' sum
 constexpr uint32_t kMaxQueryRows = DS_MAX_QUERY_ROWS;
 
@@ -15,18 +24,24 @@ void decode_plan(DecodeArgs &a)
     const uint32_t query_rows = a.group * a.tokens, unit_rows = 16 * unit_tiles(a.c.dim, query_rows);
     a.n_tiles = (uint32_t)cdiv(query_rows, unit_rows);
     a.part_rows = a.n_tiles == 1 ? query_rows : unit_rows;
+    const uint32_t key_bytes = a.c.dim * (a.c.type == DS_E4M3 ? 1 : 2);
+    a.by_slot = key_bytes <= 128;
     uint64_t blocks = cdiv(a.c.cap, kBlockTokens);
     if (a.window) {
         const uint64_t seen = cdiv(a.sinks, kBlockTokens) + cdiv((uint64_t)a.window + a.tokens + kBlockTokens - 2, kBlockTokens);
         blocks = blocks < seen ? blocks : seen;
     }
     a.score_len = (uint32_t)blocks * kBlockTokens;
+    // two steps per wave; four where a step has two tiles of query rows and
+    // only two workgroups fit a compute unit (16 rows of 1,024 visible tokens
+    // and 40 query rows: 640 workgroups in two rounds 27 us, 384 in one 19 us)
+    a.slot_blocks = unit_rows > 16 ? 16 : 8;
     // no row can be cut, or so many rows that none need be: one slot each
-    a.slot_goal = blocks > kMinSlotBlocks && a.n_rows <= kBalancedRows ? (uint32_t)cdiv(kPairGoal, a.c.n_kv) : 0;
+    a.slot_goal = blocks > a.slot_blocks && a.n_rows <= kBalancedRows ? (uint32_t)cdiv(unit_goal(key_bytes, unit_rows / 16), a.c.n_kv * a.n_tiles) : 0;
     a.n_slots = a.n_rows;
     if (a.slot_goal) {
         // ceil(total / most) <= total / most + 1 per row
-        const uint64_t most = (uint64_t)a.n_rows * cdiv(blocks, kMinSlotBlocks);
+        const uint64_t most = (uint64_t)a.n_rows * cdiv(blocks, a.slot_blocks);
         a.n_slots = (uint32_t)(a.slot_goal + a.n_rows < most ? a.slot_goal + a.n_rows : most);
     }
 }
@@ -124,6 +139,22 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t 
     const uint32_t n = length_of(a, row, req);
     const Span span = span_of(n, a.tokens, a.window, a.sinks);
     if (chunk * (kMassTokens / kBlockTokens) >= span.total) return;
+    // the scores of the first query rows and what the masses are to be added
+    // to are under way while the maxima and sums are joined
+    constexpr uint32_t kAhead = 8;
+    const uint32_t tok = chunk * kMassTokens + threadIdx.x * 4, v = tok / kBlockTokens;
+    const bool on = v < span.total;
+    const uint32_t b = v < span.sink_blocks ? v : span.first_block + (v - span.sink_blocks);
+    const uint32_t j = b * kBlockTokens + tok % kBlockTokens;
+    const float *from = a.scores + ((uint64_t)row * c.n_kv + head) * query_rows * a.score_len + tok;
+    float *to = a.mass + ((uint64_t)req * c.n_kv + head) * a.mass_len + j;
+    floatx4 ahead[kAhead], w = {0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t r = 0; r < kAhead; r++)
+        if (on && r < query_rows) ahead[r] = *reinterpret_cast<const floatx4 *>(from + (uint64_t)r * a.score_len);
+    float old[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) old[e] = on && j + e + a.tokens < n ? to[e] : 0.0f;   // the newest tokens start from 0
     const uint32_t first = a.row_slots[2 * row], count = a.row_slots[2 * row + 1];
     for (uint32_t r = threadIdx.x / 16; r < query_rows; r += 16) {
         const floatx2 ml = join_ml<16>(a.part_ml + 2 * part_at(a, first, head, r, unit_rows), stride, count);
@@ -133,22 +164,19 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t 
         }
     }
     __syncthreads();
-    const uint32_t tok = chunk * kMassTokens + threadIdx.x * 4, v = tok / kBlockTokens;
-    if (v >= span.total) return;
-    const uint32_t b = v < span.sink_blocks ? v : span.first_block + (v - span.sink_blocks);
-    const uint32_t j = b * kBlockTokens + tok % kBlockTokens;
-    const float *from = a.scores + ((uint64_t)row * c.n_kv + head) * query_rows * a.score_len + tok;
-    floatx4 w = {0, 0, 0, 0};
-#pragma unroll 4
-    for (uint32_t r = 0; r < query_rows; r++) {
-        const floatx4 s = *reinterpret_cast<const floatx4 *>(from + (uint64_t)r * a.score_len);
+    if (!on) return;
+    auto add = [&](uint32_t r, floatx4 s) {
 #pragma unroll
         for (int e = 0; e < 4; e++) w[e] += __builtin_amdgcn_exp2f(s[e] - sm_m[r]) * sm_inv[r];
-    }
-    float *to = a.mass + ((uint64_t)req * c.n_kv + head) * a.mass_len + j;
+    };
+#pragma unroll
+    for (uint32_t r = 0; r < kAhead; r++)
+        if (r < query_rows) add(r, ahead[r]);
+#pragma unroll 4
+    for (uint32_t r = kAhead; r < query_rows; r++) add(r, *reinterpret_cast<const floatx4 *>(from + (uint64_t)r * a.score_len));
 #pragma unroll
     for (int e = 0; e < 4; e++)
-        if (j + e < n) to[e] = j + e + a.tokens < n ? to[e] + w[e] : w[e];
+        if (j + e < n) to[e] = old[e] + w[e];
 }
 
 template <typename T>

@@ -37,6 +37,8 @@ struct DecodeArgs {
     uint32_t n_tiles;      // tiles per pair
     uint32_t n_slots;      // most slots of a batch of this size
     uint32_t slot_goal;    // slots wanted where the caches are long enough; 0: one per row
+    uint32_t slot_blocks;  // and blocks that are not cut further
+    bool by_slot;          // a slot's pairs on one die (attend_kernel)
     uint32_t part_rows;    // query rows of a unit's partial result
     uint32_t score_len;    // tokens of a row of scores
     float *part_o;         // (unit, part_rows, padded dim); a row in one slot has none
