@@ -1,10 +1,11 @@
 // Eviction from the paged cache by accumulated attention weight.
 //
 // Per (row, head) the kept set is a selection: the k-th largest of the masses
-// that compete is found digit by digit (8 bits from the top, counting the
-// values that agree with the digits found so far), then one walk in token
-// order keeps what is larger, and of what is equal the earliest. The copy of
-// the kept keys and values is a second launch over all tokens of all rows.
+// that compete is found digit by digit (11, 11 and 10 bits from the top,
+// counting the values that agree with the digits found so far), then one walk
+// in token order keeps what is larger, and of what is equal the earliest. The
+// copy of the kept keys and values is a second launch over all tokens of all
+// rows, and bound by memory: 16 bytes per thread, read and written once.
 #include "common.h"
 #include "serve.h"
 
@@ -12,7 +13,7 @@ namespace ds {
 
 constexpr int kSelect = 1024;              // threads of one selection
 constexpr int kSelectWaves = kSelect / 64;
-constexpr uint32_t kCopyTokens = 64;       // tokens of one workgroup of the copy
+constexpr uint32_t kCopyTokens = 32;       // tokens of one workgroup of the copy
 
 struct Cut {
     uint32_t req, n, keep;                 // keep == n: not cut
@@ -49,100 +50,217 @@ __device__ __forceinline__ uint32_t mass_key(float x)
     return (u >> 31) ? ~u : (u | 0x80000000u);
 }
 
-__global__ __launch_bounds__(kSelect) void select_kernel(const EvictArgs a)
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+
+constexpr int kBins = 2048;
+constexpr int kCopies = 4;                 // of the digit counts: sixteen lanes share one, equal masses
+                                           // (zeros are common) meet in an atomic no more often
+constexpr int kCopyPitch = kBins + 16;     // the copies of a bin lie in different banks
+constexpr int kAhead = 8;                  // groups of 64 tokens under way per wave
+constexpr uint32_t kList = 8192;           // masses with the first digit sought that fit into LDS
+struct Select {
+    uintx4 hist4[kCopyPitch * kCopies / 4];
+    uint32_t list[kList], listed, wave_total[kSelectWaves], pick[3], gt_of[kSelectWaves], eq_of[kSelectWaves];
+};
+
+// The largest digit d such that `want` of the counted values have a digit of
+// at least d: pick[0] = d, pick[1] = how many of digit d itself are wanted,
+// pick[2] = how many have it.
+__device__ inline void pick_digit(Select &sm, uint32_t want)
 {
-    __shared__ uint32_t hist[256], pick[2], gt_of[kSelectWaves], eq_of[kSelectWaves];
-    const uint32_t row = blockIdx.x / a.src.n_kv, head = blockIdx.x % a.src.n_kv;
-    const Cut x = cut_of(a, row);
-    if (threadIdx.x == 0 && head == 0) a.dst.len[row] = x.keep;
-    if (x.keep == x.n) return;
-    const float *mass = a.mass + ((uint64_t)x.req * a.src.n_kv + head) * a.mass_len;
-    uint32_t *kept = a.kept + ((uint64_t)row * a.src.n_kv + head) * a.kept_len;
-    const uint32_t lo = a.sinks, hi = x.n - a.recent;          // the tokens that compete
-    uint32_t want = x.keep - a.sinks - a.recent;               // how many of them stay
-    const int wave = threadIdx.x >> 6;
+    // thread t adds up bins 2047 - 2 t and 2046 - 2 t
+    const int wave = threadIdx.x >> 6, top = kBins - 1 - 2 * (int)threadIdx.x;
+    uint32_t h[2] = {0, 0};
+#pragma unroll
+    for (int c = 0; c < kCopies; c++) {
+        const uintx2 x = *reinterpret_cast<const uintx2 *>(reinterpret_cast<const uint32_t *>(sm.hist4) + c * kCopyPitch + top - 1);
+        h[0] += x[1];
+        h[1] += x[0];
+    }
+    const uint32_t incl = wave_incl_scan_dpp(h[0] + h[1]);
+    if (lane_id() == 63) sm.wave_total[wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - h[0] - h[1];
+    for (int w = 0; w < wave; w++) before += sm.wave_total[w];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        if (before < want && want <= before + h[k]) {
+            sm.pick[0] = top - k;
+            sm.pick[1] = want - before;
+            sm.pick[2] = h[k];
+        }
+        before += h[k];
+    }
+    __syncthreads();
+}
+
+// The selection of one (row, head) by 16 waves. Each wave owns a run of
+// tokens in groups of 64. The masses that have
+// the first digit sought are listed in LDS if they fit there, and the other
+// digits found from the list. Its time goes into the passes over the masses
+// on one compute unit (24 selections of 60,000 to 100,000 tokens 90 us; 256
+// of 2,048 to 6,144 17 us) and, for few tokens, into a chain of barriers
+// (700 tokens 9 us; with all counts of a bin in one bank 21 us).
+__device__ inline void select_tokens(const EvictArgs &a, const Cut &x, const float *mass, float *mass_out, uint32_t *kept, Select &sm)
+{
+    const uint32_t n = x.n, lo = a.sinks, span = n - a.recent - a.sinks;   // the tokens that compete
+    uint32_t want = x.keep - a.sinks - a.recent;                           // how many of them stay
+    const int wave = threadIdx.x >> 6, lane = lane_id();
+    const uint32_t run = (uint32_t)align_up(cdiv(n, kSelectWaves), 64);
+    const uint32_t w0 = wave * run < n ? wave * run : n, w1 = w0 + run < n ? w0 + run : n;
+
+    // f(token, mass) for every group of 64 tokens, one per lane, in order;
+    // tokens from n on come with any mass. The loads of kAhead groups are
+    // issued at once and without conditions, so that one wait serves them all.
+    auto groups = [&](auto &&f) {
+#pragma unroll 1
+        for (uint32_t j = w0; j < w1; j += 64 * kAhead) {
+            float v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; i++) {
+                const uint32_t at = j + i * 64 + lane;
+                v[i] = mass[at < n ? at : n - 1];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; i++)
+                if (j + i * 64 < w1) f(j + i * 64 + lane, v[i]);
+        }
+    };
+    auto clear = [&]() {
+        for (int i = threadIdx.x; i < kCopyPitch * kCopies / 4; i += kSelect) sm.hist4[i] = uintx4{0, 0, 0, 0};
+        __syncthreads();
+    };
+    auto count = [&](uint32_t digit) {
+        atomicAdd(reinterpret_cast<uint32_t *>(sm.hist4) + (lane & (kCopies - 1)) * kCopyPitch + digit, 1u);
+    };
 
     uint32_t bar = 0xFFFFFFFFu;            // the smallest kept key; of it the first `want` stay
     if (want) {
-        uint32_t found = 0;                // the digits of bar so far
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+        if (threadIdx.x == 0) sm.listed = 0;
+        clear();
+        groups([&](uint32_t j, float v) {
+            if (j - lo < span) count(mass_key(v) >> 21);
+        });
+        __syncthreads();
+        pick_digit(sm, want);
+        uint32_t found = sm.pick[0];       // the digits of bar so far
+        want = sm.pick[1];
+        const bool fits = sm.pick[2] <= kList;
+        if (fits) {
+            groups([&](uint32_t j, float v) {
+                const uint32_t key = mass_key(v);
+                const bool on = j - lo < span && key >> 21 == found;
+                const uint64_t all = __ballot(on);
+                if (!all) return;
+                uint32_t to = 0;
+                if (lane == 0) to = atomicAdd(&sm.listed, (uint32_t)__popcll(all));
+                to = readlane32(to, 0) + (uint32_t)__popcll(all & lanemask_lt());
+                if (on) sm.list[to] = key;
+            });
             __syncthreads();
-            for (uint32_t j = lo + threadIdx.x; j < hi; j += kSelect) {
-                const uint32_t key = mass_key(mass[j]);
-                if (shift == 24 || (key >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255u], 1u);
-            }
+        }
+#pragma unroll 1
+        for (int shift = 10; shift >= 0; shift -= 10) {
+            // bits 20 .. 10, then 9 .. 0
+            const uint32_t mask = shift ? 2047u : 1023u;
+            const int above = shift ? 21 : 10;
+            clear();
+            auto look = [&](uint32_t key) {
+                if (key >> above == found) count((key >> shift) & mask);
+            };
+            if (fits)
+                for (uint32_t i = threadIdx.x; i < sm.listed; i += kSelect) look(sm.list[i]);
+            else
+                groups([&](uint32_t j, float v) {
+                    if (j - lo < span) look(mass_key(v));
+                });
             __syncthreads();
-            if (wave == 0) {
-                // lane l holds digits 255 - 4 l .. 252 - 4 l: counts from the largest digit down
-                uint32_t h[4], own = 0;
-#pragma unroll
-                for (int k = 0; k < 4; k++) own += h[k] = hist[255 - 4 * lane_id() - k];
-                uint32_t before = wave_incl_scan_dpp(own) - own;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    if (before < want && want <= before + h[k]) {
-                        pick[0] = 255 - 4 * lane_id() - k;
-                        pick[1] = want - before;
-                    }
-                    before += h[k];
-                }
-            }
-            __syncthreads();
-            found |= pick[0] << shift;
-            want = pick[1];
-            __syncthreads();
+            pick_digit(sm, want);
+            found = found << (shift ? 11 : 10) | sm.pick[0];
+            want = sm.pick[1];
         }
         bar = found;
     }
 
-    // kept tokens in their order: each wave walks a run of its own
-    const uint32_t run = (uint32_t)align_up(cdiv(x.n, kSelectWaves), 64);
-    const uint32_t j0 = wave * run < x.n ? wave * run : x.n, j1 = j0 + run < x.n ? j0 + run : x.n;
-    uint32_t n_gt = 0, n_eq = 0;
-    auto state = [&](uint32_t j, bool &gt, bool &eq) {
-        const bool in = j < j1, sure = in && (j < lo || j >= hi);
-        const uint32_t key = in && !sure ? mass_key(mass[j]) : 0u;
-        gt = sure || (in && key > bar);
-        eq = in && !sure && want && key == bar;
+    // kept tokens in their order: of every wave's run how many, then where
+    auto state = [&](uint32_t j, float v, bool &gt, bool &eq) {
+        const uint32_t key = mass_key(v);
+        const bool competes = j - lo < span;
+        gt = competes ? key > bar : j < n;
+        eq = competes && want && key == bar;
     };
-    for (uint32_t j = j0; j < j1; j += 64) {
+    uint32_t n_gt = 0, n_eq = 0;
+    groups([&](uint32_t j, float v) {
         bool gt, eq;
-        state(j + lane_id(), gt, eq);
-        n_gt += __popcll(__ballot(gt));
-        n_eq += __popcll(__ballot(eq));
-    }
-    if (lane_id() == 0) {
-        gt_of[wave] = n_gt;
-        eq_of[wave] = n_eq;
+        state(j, v, gt, eq);
+        n_gt += (uint32_t)__popcll(__ballot(gt));
+        n_eq += (uint32_t)__popcll(__ballot(eq));
+    });
+    if (lane == 0) {
+        sm.gt_of[wave] = n_gt;
+        sm.eq_of[wave] = n_eq;
     }
     __syncthreads();
     uint32_t at = 0, eq_at = 0;
     for (int w = 0; w < wave; w++) {
         const uint32_t left = eq_at < want ? want - eq_at : 0;
-        at += gt_of[w] + (eq_of[w] < left ? eq_of[w] : left);
-        eq_at += eq_of[w];
+        at += sm.gt_of[w] + (sm.eq_of[w] < left ? sm.eq_of[w] : left);
+        eq_at += sm.eq_of[w];
     }
-    for (uint32_t j = j0; j < j1; j += 64) {
-        bool gt, eq;
-        state(j + lane_id(), gt, eq);
-        const uint64_t eqs = __ballot(eq);
-        const bool stays = gt || (eq && eq_at + __popcll(eqs & lanemask_lt()) < want);
+    const bool direct = mass_out != mass;
+    groups([&](uint32_t j, float v) {
+        bool stays, eq;
+        state(j, v, stays, eq);
+        if (const uint64_t eqs = __ballot(eq)) {
+            stays = stays || (eq && eq_at + (uint32_t)__popcll(eqs & lanemask_lt()) < want);
+            eq_at += (uint32_t)__popcll(eqs);
+        }
         const uint64_t all = __ballot(stays);
-        if (stays) kept[at + __popcll(all & lanemask_lt())] = j + lane_id();
-        at += __popcll(all);
-        eq_at += __popcll(eqs);
-    }
+        const uint32_t to = at + (uint32_t)__popcll(all & lanemask_lt());
+        if (stays) {
+            kept[to] = j;
+            if (direct) mass_out[to] = v;
+        }
+        at += (uint32_t)__popcll(all);
+    });
+    if (direct) return;
+    // kept[i] >= i: reading a piece before writing it is enough
     __syncthreads();
-    // kept[i] >= i: reading a piece before writing it is enough where mass_out is mass
-    float *mass_out = a.mass_out + ((uint64_t)x.req * a.src.n_kv + head) * a.mass_len;
-    for (uint32_t i = 0; i < x.keep; i += kSelect) {
-        const uint32_t k = i + threadIdx.x;
-        const float val = k < x.keep ? mass[kept[k]] : 0.0f;
+    constexpr int kPiece = 8;
+    for (uint32_t i = 0; i < x.keep; i += kSelect * kPiece) {
+        float v[kPiece];
+#pragma unroll
+        for (int k = 0; k < kPiece; k++) {
+            const uint32_t p = i + k * kSelect + threadIdx.x;
+            v[k] = p < x.keep ? mass[kept[p]] : 0.0f;
+        }
         __syncthreads();
-        if (k < x.keep) mass_out[k] = val;
+#pragma unroll
+        for (int k = 0; k < kPiece; k++) {
+            const uint32_t p = i + k * kSelect + threadIdx.x;
+            if (p < x.keep) mass_out[p] = v[k];
+        }
         __syncthreads();
     }
+}
+
+__global__ __launch_bounds__(kSelect) void select_kernel(const EvictArgs a)
+{
+    __shared__ Select sm;
+    const uint32_t row = blockIdx.x / a.src.n_kv, head = blockIdx.x % a.src.n_kv;
+    const Cut x = cut_of(a, row);
+    if (threadIdx.x == 0 && head == 0) a.dst.len[row] = x.keep;
+    if (x.keep == x.n) return;
+    const uint64_t of = ((uint64_t)x.req * a.src.n_kv + head) * a.mass_len;
+    uint32_t *kept = a.kept + ((uint64_t)row * a.src.n_kv + head) * a.kept_len;
+    select_tokens(a, x, a.mass + of, a.mass_out + of, kept, sm);
+}
+
+// 16 bytes, past the caches: nothing is read twice.
+__device__ __forceinline__ void put(uint8_t *to, const uint8_t *from)
+{
+    __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const uintx4 *>(from)), reinterpret_cast<uintx4 *>(to));
 }
 
 // 16 bytes of a key or value per thread and step.
@@ -163,8 +281,8 @@ __global__ __launch_bounds__(256) void copy_kernel(const EvictArgs a, uint32_t c
         if (sp >= s.n_pages || dp >= d.n_pages) continue;
         const uint64_t sa = (sp * s.page_stride + (from % s.page_size) * s.token_stride + head * s.head_stride) * elem + u * 16;
         const uint64_t da = (dp * d.page_stride + (to % d.page_size) * d.token_stride + head * d.head_stride) * elem + u * 16;
-        *reinterpret_cast<uint4 *>(d.k + da) = *reinterpret_cast<const uint4 *>(s.k + sa);
-        *reinterpret_cast<uint4 *>(d.v + da) = *reinterpret_cast<const uint4 *>(s.v + sa);
+        put(d.k + da, s.k + sa);
+        put(d.v + da, s.v + sa);
     }
 }
 

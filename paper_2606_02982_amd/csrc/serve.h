@@ -69,7 +69,8 @@ struct VerifyArgs {
     uint64_t t_row, t_pos, d_row, d_pos;
     uint32_t n_rows, n_drafts, vocab, n_requests;
     int type;
-    double *sums;          // (row, chunk, 2)
+    double *sums;          // (row, chunk, 2): of the weights and of the target
+    uint32_t *accepted;    // per row
 };
 
 constexpr uint32_t kBlockTokens = 32;   // tokens of one step of the attention loop

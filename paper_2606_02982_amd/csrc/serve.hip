@@ -162,7 +162,7 @@ ds_status ds_cache_evict(const ds_kv_cache *src, const ds_kv_cache *dst, const d
     if (params->mass_len < a.src.cap) return DS_ERR_ARG;
     if (n_rows == 0) return DS_OK;
     if (n_rows > a.dst.n_requests || (!rows && n_rows > a.src.n_requests)) return DS_ERR_ARG;
-    if ((uint64_t)n_rows * a.src.n_kv * (a.src.cap / 64 + 1) > kMaxGrid) return DS_ERR_SIZE;
+    if ((uint64_t)n_rows * a.src.n_kv * (a.src.cap / 32 + 1) > kMaxGrid) return DS_ERR_SIZE;
     st = pointers_of(a.src);
     if (st == DS_OK) st = pointers_of(a.dst);
     if (st != DS_OK) return st;
