@@ -573,38 +573,41 @@ def simulate_multi(arrival, tier, counts, category, tenant, group, observed, t_b
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
 
 
-def _on(device, **tensors):
-    """Device and type of a call's tensors: every one on ``device``, which is
-    the current one (the stream is torch's current stream there)."""
-    if device.type != "cuda":
+def _stream_on(index):
+    """Torch's current stream on device ``index`` as a number."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _device_of(t):
+    """The index of t's device, which has to be the current one (work goes to
+    torch's current stream there)."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError("the tensors must be device tensors")
-    if device.index != torch.cuda.current_device():
-        raise ValueError("the tensors are on %s, which is not the current device" % device)
-    for name, (t, dtype) in tensors.items():
-        if t is None:
-            continue
-        if t.device != device:
-            raise ValueError("%s must be on %s" % (name, device))
-        if t.dtype != dtype:
-            raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if index != torch.cuda.current_device():
+        raise ValueError("the tensors are on device %d, which is not the current one" % index)
+    return index
 
 
-def _whole(**tensors):
-    for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            raise ValueError("%s must be contiguous" % name)
-
-
-def _shaped(t, shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _arg(t, index, dtype, shape, name):
+    """The address of a contiguous tensor argument, None for none. ``shape``
+    None: any."""
+    if t is None:
+        return None
+    if t.get_device() != index or t.dtype != dtype:
+        raise ValueError("%s must be %s on device %d, got %s on %s" % (name, dtype, index, t.dtype, t.device))
+    if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
 
 
-def _scratch(ws, need, device):
+def _scratch(ws, need, like):
     """The caller's workspace, or one of this call alone: taken from torch's
     allocator on the current stream, so calls on other streams and in captured
     graphs share nothing with it."""
-    return torch.empty(max(need, 256), dtype=torch.uint8, device=device) if ws is None else ws
+    return like.new_empty(max(need, 256), dtype=torch.uint8) if ws is None else ws
 
 
 class Cache:
@@ -613,7 +616,8 @@ class Cache:
     def __init__(self, k, v, table, lens, k_scale, v_scale):
         self.k, self.v, self.table, self.lens = k, v, table, lens
         self.k_scale, self.v_scale = k_scale, v_scale
-        self.device = k.device
+        self.dtype, self.index = k.dtype, k.get_device()
+        self.n_requests, self.n_kv, self.head_dim = table.shape[0], k.shape[2], k.shape[3]
         s = self.struct = KvCache()
         s.k, s.v, s.table, s.len = k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr()
         s.k_scale = k_scale.data_ptr() if k_scale is not None else None
@@ -643,18 +647,20 @@ def kv_cache(k, v, table, lens, k_scale=None, v_scale=None):
         raise ValueError("the last axis of k and v must be dense")
     if table.dim() != 2:
         raise ValueError("table must be (n_requests, max_pages)")
-    _shaped(lens, (table.shape[0],), "lens")
-    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-        _shaped(t, (k.shape[2],), name)
-    f32, i32 = torch.float32, torch.int32
-    _on(k.device, v=(v, k.dtype), table=(table, i32), lens=(lens, i32), k_scale=(k_scale, f32), v_scale=(v_scale, f32))
-    _whole(table=table, lens=lens, k_scale=k_scale, v_scale=v_scale)
+    dev = _device_of(k)
+    if v.get_device() != dev:
+        raise ValueError("k and v must be on one device")
+    _arg(table, dev, torch.int32, None, "table")
+    _arg(lens, dev, torch.int32, table.shape[:1], "lens")
+    _arg(k_scale, dev, torch.float32, k.shape[2:3], "k_scale")
+    _arg(v_scale, dev, torch.float32, k.shape[2:3], "v_scale")
     return Cache(k, v, table, lens, k_scale, v_scale)
 
 
-def _mass_of(mass, cache, name):
-    if mass is not None and (mass.dim() != 3 or mass.shape[:2] != (cache.struct.n_requests, cache.struct.n_kv)):
-        raise ValueError("%s must be (n_requests, n_kv, length)" % name)
+def _mass_shape(mass, cache):
+    if mass.dim() != 3 or mass.shape[0] != cache.n_requests or mass.shape[1] != cache.n_kv:
+        raise ValueError("mass must be (n_requests, n_kv, length)")
+    return mass.shape
 
 
 def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len=0, mass=None, out=None, ws=None,
@@ -670,27 +676,27 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
     the batch holds, if known (a tighter launch and workspace). ``mass``:
     float32 (n_requests, n_kv, length >= max_len), updated in place with the
     weight each cached token received. Returns out, shaped like q."""
-    if q.dim() != 4 or q.shape[3] != cache.struct.head_dim or q.stride(3) != 1:
+    if q.dim() != 4 or q.shape[3] != cache.head_dim or q.stride(3) != 1:
         raise ValueError("q must be (n_rows, n_tokens, n_q, head_dim) with a dense last axis")
-    if q.dtype not in (torch.float16, torch.bfloat16):
+    if q.dtype is not torch.bfloat16 and q.dtype is not torch.float16:
         raise ValueError("q must be float16 or bfloat16, got %s" % q.dtype)
-    n, t, h, d = q.shape
+    dev = _device_of(q)
+    if dev != cache.index:
+        raise ValueError("q and the cache must be on one device")
+    n, t, h, d = shape = q.shape
     if out is None:
-        out = torch.empty((n, t, h, d), dtype=q.dtype, device=q.device)
-    _on(cache.device, q=(q, q.dtype), rows=(rows, torch.int32), mass=(mass, torch.float32), out=(out, q.dtype),
-        ws=(ws, torch.uint8))
-    _whole(rows=rows, mass=mass, out=out, ws=ws)
-    _shaped(rows, (n,), "rows")
-    _shaped(out, (n, t, h, d), "out")
-    _mass_of(mass, cache, "mass")
-    p = DecodeParams(h, t, DTYPES[q.dtype], q.stride(0), q.stride(1), q.stride(2),
-                     d ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(max_len),
-                     mass.shape[2] if mass is not None else 0)
-    ref = ctypes.byref(p)
+        out = q.new_empty(shape)
+    p_rows = _arg(rows, dev, torch.int32, shape[:1], "rows")
+    p_out = _arg(out, dev, q.dtype, shape, "out")
+    p_mass = None if mass is None else _arg(mass, dev, torch.float32, _mass_shape(mass, cache), "mass")
+    s_row, s_token, s_head, _ = q.stride()
+    p = ctypes.byref(DecodeParams(h, t, DTYPES[q.dtype], s_row, s_token, s_head, d ** -0.5 if scale is None else float(scale),
+                                  int(window), int(sinks), int(max_len), 0 if mass is None else mass.shape[2]))
     if n:
-        ws = _scratch(ws, lib.ds_decode_workspace_bytes(cache.ref, ref, n, mass is not None), q.device)
-    _check(lib.ds_decode_attention(cache.ref, ref, n, _ptr(rows), _ptr(q), _ptr(out), _ptr(mass), _ptr(ws),
-                                   ws.numel() if ws is not None else 0, _flags(validate), _stream()))
+        ws = _scratch(ws, lib.ds_decode_workspace_bytes(cache.ref, p, n, mass is not None), q)
+    p_ws = _arg(ws, dev, torch.uint8, None, "ws")
+    _check(lib.ds_decode_attention(cache.ref, p, n, p_rows, q.data_ptr(), p_out, p_mass, p_ws, 0 if ws is None else ws.numel(),
+                                   _flags(validate), _stream_on(dev)))
     return out
 
 
@@ -705,28 +711,27 @@ def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0
     ``score``. ``mass``: as ``decode_attention`` leaves it. ``mass_out``: None
     updates mass in place. ``kept``: int32 (n_rows, n_kv, length); by default
     as long as dst's rows. Returns (dst.lens, kept)."""
-    n = dst.struct.n_requests if rows is None else rows.numel()
+    dev = _device_of(budget)
+    if dev != cache.index or dev != dst.index:
+        raise ValueError("budget and the caches must be on one device")
+    n = dst.n_requests if rows is None else rows.numel()
     if mass_out is None:
         mass_out = mass
     if kept is None:
-        kept = torch.empty((n, dst.struct.n_kv, dst.struct.max_pages * dst.struct.page_size), dtype=torch.int32,
-                           device=cache.device)
-    f32, i32 = torch.float32, torch.int32
-    _on(cache.device, dst=(dst.k, cache.k.dtype), budget=(budget, torch.float64), mass=(mass, f32), mass_out=(mass_out, f32),
-        kept=(kept, i32), rows=(rows, i32), ws=(ws, torch.uint8))
-    _whole(budget=budget, mass=mass, mass_out=mass_out, kept=kept, rows=rows, ws=ws)
-    _shaped(budget, (cache.struct.n_requests,), "budget")
-    _shaped(rows, (n,), "rows")
-    _mass_of(mass, cache, "mass")
-    _shaped(mass_out, mass.shape, "mass_out")
-    if kept.dim() != 3 or kept.shape[:2] != (n, dst.struct.n_kv):
+        kept = mass.new_empty((n, dst.n_kv, dst.struct.max_pages * dst.struct.page_size), dtype=torch.int32)
+    if kept.dim() != 3 or kept.shape[0] != n or kept.shape[1] != dst.n_kv:
         raise ValueError("kept must be (n_rows, n_kv, length)")
+    p_rows = _arg(rows, dev, torch.int32, (n,), "rows")
+    p_budget = _arg(budget, dev, torch.float64, (cache.n_requests,), "budget")
+    p_mass = _arg(mass, dev, torch.float32, _mass_shape(mass, cache), "mass")
+    p_out = _arg(mass_out, dev, torch.float32, mass.shape, "mass_out")
+    p_kept = _arg(kept, dev, torch.int32, None, "kept")
     p = EvictParams(int(sinks), int(recent), int(slack), int(max_len), mass.shape[2], kept.shape[2])
     if validate:
-        ws = _scratch(ws, 256, cache.device)
-    _check(lib.ds_cache_evict(cache.ref, dst.ref, ctypes.byref(p), n, _ptr(rows), _ptr(budget), _ptr(mass),
-                              _ptr(mass_out), _ptr(kept), _ptr(ws), ws.numel() if ws is not None else 0,
-                              _flags(validate), _stream()))
+        ws = _scratch(ws, 256, mass)
+    p_ws = _arg(ws, dev, torch.uint8, None, "ws")
+    _check(lib.ds_cache_evict(cache.ref, dst.ref, ctypes.byref(p), n, p_rows, p_budget, p_mass, p_out, p_kept, p_ws,
+                              0 if ws is None else ws.numel(), _flags(validate), _stream_on(dev)))
     return dst.lens, kept
 
 
@@ -741,43 +746,45 @@ def verify_draft(target, draft, tokens, u, u_sample, n_draft=None, rows=None, ob
     (n_rows, n_drafts), ``u_sample``: float32 (n_rows), uniform in [0, 1).
     ``observed``, ``lens``: int32 (n_requests), updated in place at ``rows``.
     Returns (out, n_emitted): int32 (n_rows, n_drafts + 1) and (n_rows)."""
-    if target.dim() != 3 or target.stride(2) != 1 or target.dtype not in (torch.float32, torch.float16, torch.bfloat16):
+    kind = DTYPES.get(target.dtype, 3)
+    if target.dim() != 3 or target.stride(2) != 1 or kind == 3:
         raise ValueError("target must be (n_rows, n_drafts + 1, vocab), float32, float16 or bfloat16, the last axis dense")
-    n, k, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
+    n, k, vocab = target.shape
+    k -= 1
     if k < 0:
         raise ValueError("target needs at least one position")
     if draft is not None:
-        _shaped(draft, (n, k, vocab), "draft")
+        if draft.shape != (n, k, vocab) or draft.dtype != target.dtype:
+            raise ValueError("draft must be %s of shape %s, got %s of %s" % (target.dtype, (n, k, vocab), draft.dtype, tuple(draft.shape)))
         if draft.numel() == 0:
             draft = None
         elif draft.stride(2) != 1:
             raise ValueError("the last axis of draft must be dense")
-    dev, i32, f32 = target.device, torch.int32, torch.float32
+    dev, i32, f32 = _device_of(target), torch.int32, torch.float32
+    if draft is not None and draft.get_device() != dev:
+        raise ValueError("draft must be on the target's device")
     if out is None:
-        out = torch.empty((n, k + 1), dtype=i32, device=dev)
+        out = target.new_empty((n, k + 1), dtype=i32)
     if n_emitted is None:
-        n_emitted = torch.empty(n, dtype=i32, device=dev)
-    _on(dev, target=(target, target.dtype), draft=(draft, target.dtype), tokens=(tokens, i32), u=(u, f32),
-        u_sample=(u_sample, f32), n_draft=(n_draft, i32), rows=(rows, i32), observed=(observed, i32), lens=(lens, i32),
-        out=(out, i32), n_emitted=(n_emitted, i32), ws=(ws, torch.uint8))
-    _whole(tokens=tokens, u=u, u_sample=u_sample, n_draft=n_draft, rows=rows, observed=observed, lens=lens, out=out,
-           n_emitted=n_emitted, ws=ws)
-    for t, shape, name in ((tokens, (n, k), "tokens"), (u, (n, k), "u"), (u_sample, (n,), "u_sample"), (rows, (n,), "rows"),
-                           (n_draft, (n,), "n_draft"), (out, (n, k + 1), "out"), (n_emitted, (n,), "n_emitted")):
-        _shaped(t, shape, name)
-    n_req = n
-    for t, name in ((observed, "observed"), (lens, "lens")):
-        if t is not None:
-            n_req = t.numel()
-            _shaped(t, (n_req,), name)
-    if observed is not None and lens is not None:
-        _shaped(lens, observed.shape, "lens")
-    p = VerifyParams(k, vocab, n_req, DTYPES[target.dtype], target.stride(0), target.stride(1),
-                     draft.stride(0) if draft is not None else 0, draft.stride(1) if draft is not None else 0)
-    ref = ctypes.byref(p)
+        n_emitted = target.new_empty(n, dtype=i32)
+    at = lens if observed is None else observed
+    n_req = n if at is None else at.numel()
+    p_tokens = _arg(tokens, dev, i32, (n, k), "tokens")
+    p_u = _arg(u, dev, f32, (n, k), "u")
+    p_sample = _arg(u_sample, dev, f32, (n,), "u_sample")
+    p_draft = _arg(n_draft, dev, i32, (n,), "n_draft")
+    p_rows = _arg(rows, dev, i32, (n,), "rows")
+    p_observed = _arg(observed, dev, i32, (n_req,), "observed")
+    p_lens = _arg(lens, dev, i32, (n_req,), "lens")
+    p_out = _arg(out, dev, i32, (n, k + 1), "out")
+    p_emitted = _arg(n_emitted, dev, i32, (n,), "n_emitted")
+    t_row, t_pos, _ = target.stride()
+    d_row, d_pos, _ = (0, 0, 0) if draft is None else draft.stride()
+    p = ctypes.byref(VerifyParams(k, vocab, n_req, kind, t_row, t_pos, d_row, d_pos))
     if n:
-        ws = _scratch(ws, lib.ds_verify_workspace_bytes(ref, n), dev)
-    _check(lib.ds_verify_draft(ref, n, _ptr(rows), _ptr(target), _ptr(draft), _ptr(tokens), _ptr(n_draft), _ptr(u),
-                               _ptr(u_sample), _ptr(out), _ptr(n_emitted), _ptr(observed), _ptr(lens), _ptr(ws),
-                               ws.numel() if ws is not None else 0, _flags(validate), _stream()))
+        ws = _scratch(ws, lib.ds_verify_workspace_bytes(p, n), target)
+    p_ws = _arg(ws, dev, torch.uint8, None, "ws")
+    _check(lib.ds_verify_draft(p, n, p_rows, target.data_ptr(), None if draft is None else draft.data_ptr(), p_tokens, p_draft,
+                               p_u, p_sample, p_out, p_emitted, p_observed, p_lens, p_ws, 0 if ws is None else ws.numel(),
+                               _flags(validate), _stream_on(dev)))
     return out, n_emitted
