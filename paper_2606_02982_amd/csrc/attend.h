@@ -583,16 +583,25 @@ void attend_kernel(const DecodeArgs a)
     const int lane = lane_id(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     // Workgroups go round the eight dies, each with a cache of its own. Units
-    // of one pair, which read the same keys and values, go to one die; so do
-    // all heads of a slot where a token's key is at most 128 bytes, a cache
-    // line (8-bit, 8 heads: 64 dimensions 92 -> 69 us for 268 MB, 128
-    // dimensions 119 -> 116 us for 537 MB; 16-bit, 128 dimensions the other
-    // way round: 198 -> 202 us for 1.07 GB).
-    const uint32_t of_slot = a.by_slot ? c.n_kv : 1;
+    // of one pair, which read the same keys and values, go to one die. Which
+    // pairs are under way at one time:
+    //  - all heads of a slot on one die where a token's key is at most 128
+    //    bytes, a cache line (8-bit, 8 heads: 64 dimensions 92 -> 69 us for
+    //    268 MB, 128 dimensions 119 -> 116 us for 537 MB);
+    //  - all slots of few heads, up to 8 heads (8 heads of 128 dimensions in
+    //    16 bits: 192 -> 177 us for 1.07 GB, three long rows 241 -> 222 us
+    //    for 1.33 GB); the odd number of slots spreads a slot's heads over
+    //    the dies;
+    //  - else all heads of few slots (16 heads: ragged rows up to 2,048 62 us
+    //    for 292 MB, slots first 62 to 83; long rows 371 and 357 us).
+    const uint32_t of_slot = a.spread == kDieOfSlot ? c.n_kv : 1;
     const uint32_t round = blockIdx.x / (8 * a.n_tiles * of_slot), within = blockIdx.x % (8 * a.n_tiles * of_slot);
     const uint32_t tile = within / 8 % a.n_tiles;
-    const uint32_t pair = (round * 8 + within % 8) * of_slot + within / 8 / a.n_tiles;
-    const uint32_t slot = pair / c.n_kv, head = pair % c.n_kv;
+    const uint32_t at = (round * 8 + within % 8) * of_slot + within / 8 / a.n_tiles, per_head = a.n_slots | 1;
+    const uint32_t slot = a.spread == kSlotsFirst ? at % per_head : at / c.n_kv;
+    const uint32_t head = a.spread == kSlotsFirst ? at / per_head : at % c.n_kv;
+    if (slot >= a.n_slots || head >= c.n_kv) return;
+    const uint32_t pair = slot * c.n_kv + head;
     const Slots slots = find_slots(a, slot);
     const uint32_t row = slots.row;
     if (row == kNone) return;
@@ -706,8 +715,7 @@ void attend_kernel(const DecodeArgs a)
 template <typename T, bool kE4m3, int kDim, int kTiles, bool kStream>
 hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
 {
-    const uint64_t groups = a.by_slot ? a.n_slots : (uint64_t)a.n_slots * a.c.n_kv;
-    const uint64_t grid = cdiv(groups, 8) * 8 * a.n_tiles * (a.by_slot ? a.c.n_kv : 1);
+    const uint64_t grid = attend_grid(a);
     // lane offsets in half a block take 32 bits
     if (a.c.page_size % 16 == 0 && a.c.dim == kDim && a.c.token_stride < (1u << 26))
         attend_kernel<T, kE4m3, kDim, kTiles, true, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);

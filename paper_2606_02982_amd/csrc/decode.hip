@@ -25,7 +25,7 @@ void decode_plan(DecodeArgs &a)
     a.n_tiles = (uint32_t)cdiv(query_rows, unit_rows);
     a.part_rows = a.n_tiles == 1 ? query_rows : unit_rows;
     const uint32_t key_bytes = a.c.dim * (a.c.type == DS_E4M3 ? 1 : 2);
-    a.by_slot = key_bytes <= 128;
+    a.spread = key_bytes <= 128 ? kDieOfSlot : a.c.n_kv <= 8 ? kSlotsFirst : kHeadsFirst;
     uint64_t blocks = cdiv(a.c.cap, kBlockTokens);
     if (a.window) {
         const uint64_t seen = cdiv(a.sinks, kBlockTokens) + cdiv((uint64_t)a.window + a.tokens + kBlockTokens - 2, kBlockTokens);

@@ -38,7 +38,7 @@ struct DecodeArgs {
     uint32_t n_slots;      // most slots of a batch of this size
     uint32_t slot_goal;    // slots wanted where the caches are long enough; 0: one per row
     uint32_t slot_blocks;  // and blocks that are not cut further
-    bool by_slot;          // a slot's pairs on one die (attend_kernel)
+    int spread;            // order of the pairs (attend_kernel)
     uint32_t part_rows;    // query rows of a unit's partial result
     uint32_t score_len;    // tokens of a row of scores
     float *part_o;         // (unit, part_rows, padded dim); a row in one slot has none
@@ -94,6 +94,15 @@ __host__ __device__ inline Span span_of(uint32_t n, uint32_t tokens, uint32_t wi
     s.sink_blocks = sb < s.first_block ? sb : s.first_block;
     s.total = s.sink_blocks + (n + kBlockTokens - 1) / kBlockTokens - s.first_block;
     return s;
+}
+
+enum { kHeadsFirst, kSlotsFirst, kDieOfSlot };   // DecodeArgs.spread
+
+// Workgroups of the attention kernel.
+inline uint64_t attend_grid(const DecodeArgs &a)
+{
+    const uint64_t n_kv = a.c.n_kv, slots = a.spread == kSlotsFirst ? a.n_slots | 1u : a.n_slots;
+    return a.spread == kDieOfSlot ? (slots + 7) / 8 * 8 * n_kv * a.n_tiles : (slots * n_kv + 7) / 8 * 8 * a.n_tiles;
 }
 
 // Sets the split of a; the largest grid and the workspace bytes follow from it.

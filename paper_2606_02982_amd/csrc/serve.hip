@@ -86,7 +86,7 @@ ds_status decode_args(const ds_kv_cache *cache, const ds_decode_params *p, uint3
     if (n_rows == 0) return DS_OK;
     if (n_rows > DS_MAX_ITEMS || (uint64_t)n_rows * a.c.n_kv * a.group * a.tokens > kMaxGrid) return DS_ERR_SIZE;
     decode_plan(a);
-    if (((uint64_t)a.n_slots + 8) * a.c.n_kv * a.n_tiles + 8 * a.n_tiles > kMaxGrid ||
+    if (attend_grid(a) > kMaxGrid ||
         (uint64_t)n_rows * a.c.n_kv * (a.score_len / 1024 + 2 + a.group * a.tokens) > kMaxGrid)
         return DS_ERR_SIZE;
     return DS_OK;
