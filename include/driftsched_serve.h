@@ -161,13 +161,16 @@ typedef struct {
  *             else is written
  * A row whose keep exceeds kept_len or dst's max_pages * page_size is not cut
  * (DS_VALIDATE reports it). A request may stand in one row only.
- *  ws         workspace of 256 bytes (used by DS_VALIDATE only; may be NULL
- *             without that flag)
+ *  ws         workspace of ds_evict_workspace_bytes(src, dst, params, n_rows)
  */
 ds_status ds_cache_evict(const ds_kv_cache *src, const ds_kv_cache *dst,
                          const ds_evict_params *params, uint32_t n_rows, const uint32_t *rows,
                          const double *budget, const float *mass, float *mass_out, uint32_t *kept,
                          void *ws, size_t ws_bytes, uint32_t flags, ds_stream stream);
+
+/* Workspace of ds_cache_evict; 0 if it would refuse the structs. */
+size_t ds_evict_workspace_bytes(const ds_kv_cache *src, const ds_kv_cache *dst,
+                                const ds_evict_params *params, uint32_t n_rows);
 
 /* Parameters of ds_verify_draft. */
 typedef struct {

@@ -25,7 +25,6 @@ void decode_plan(DecodeArgs &a)
     a.n_tiles = (uint32_t)cdiv(query_rows, unit_rows);
     a.part_rows = a.n_tiles == 1 ? query_rows : unit_rows;
     const uint32_t key_bytes = a.c.dim * (a.c.type == DS_E4M3 ? 1 : 2);
-    a.spread = key_bytes <= 128 ? kDieOfSlot : a.c.n_kv <= 8 ? kSlotsFirst : kHeadsFirst;
     uint64_t blocks = cdiv(a.c.cap, kBlockTokens);
     if (a.window) {
         const uint64_t seen = cdiv(a.sinks, kBlockTokens) + cdiv((uint64_t)a.window + a.tokens + kBlockTokens - 2, kBlockTokens);
@@ -44,6 +43,8 @@ void decode_plan(DecodeArgs &a)
         const uint64_t most = (uint64_t)a.n_rows * cdiv(blocks, a.slot_blocks);
         a.n_slots = (uint32_t)(a.slot_goal + a.n_rows < most ? a.slot_goal + a.n_rows : most);
     }
+    // a die per slot needs slots for every die
+    a.spread = key_bytes <= 128 && a.n_slots >= 64 ? kDieOfSlot : a.c.n_kv <= 8 ? kSlotsFirst : kHeadsFirst;
 }
 
 static uint64_t part_rows_of(const DecodeArgs &a) { return (uint64_t)a.n_slots * a.c.n_kv * a.n_tiles * a.part_rows; }

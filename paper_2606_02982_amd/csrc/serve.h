@@ -56,6 +56,13 @@ struct EvictArgs {
     uint32_t *kept;
     uint64_t mass_len, kept_len;
     uint32_t n_rows, sinks, recent, slack;
+    // long requests: the selection split into chunks of tokens
+    uint32_t chunk_tokens, n_chunks;   // n_chunks 0: one workgroup selects for a (row, head)
+    uint32_t most_kept;                // the most tokens that a request can keep
+    uint32_t *counts;                  // (row, head, chunk, 2048): masses by their first digit
+    uint32_t *starts;                  // (row, head, chunk, 2): kept and equal tokens before the chunk
+    uint32_t *bars;                    // (row, head, 2): smallest kept key, how many of it stay
+    float *kept_mass;                  // (row, head, most_kept)
 };
 
 struct VerifyArgs {
@@ -118,7 +125,10 @@ hipError_t decode_attend_f16(const DecodeArgs &a, hipStream_t s);
 hipError_t decode_attend_bf16_e4m3(const DecodeArgs &a, hipStream_t s);
 hipError_t decode_attend_f16_e4m3(const DecodeArgs &a, hipStream_t s);
 
-hipError_t evict_launch(const EvictArgs &a, hipStream_t s);
+// Sets the chunks of a.
+void evict_plan(EvictArgs &a);
+size_t evict_ws_bytes(const EvictArgs &a);
+hipError_t evict_launch(EvictArgs a, void *ws, hipStream_t s);
 hipError_t evict_check(const EvictArgs &a, uint32_t *flag, hipStream_t s);
 
 size_t verify_ws_bytes(uint32_t n_rows, uint32_t vocab);

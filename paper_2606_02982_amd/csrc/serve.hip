@@ -92,6 +92,29 @@ ds_status decode_args(const ds_kv_cache *cache, const ds_decode_params *p, uint3
     return DS_OK;
 }
 
+ds_status evict_args(const ds_kv_cache *src, const ds_kv_cache *dst, const ds_evict_params *params, uint32_t n_rows, EvictArgs &a)
+{
+    if (!params) return DS_ERR_NULL;
+    a = EvictArgs{};
+    ds_status st = view_of(src, params->max_len, a.src);
+    if (st == DS_OK) st = view_of(dst, 0, a.dst);
+    if (st != DS_OK) return st;
+    if (a.src.type != a.dst.type || a.src.page_size != a.dst.page_size || a.src.n_kv != a.dst.n_kv || a.src.dim != a.dst.dim ||
+        a.src.page_stride != a.dst.page_stride || a.src.token_stride != a.dst.token_stride ||
+        a.src.head_stride != a.dst.head_stride)
+        return DS_ERR_ARG;
+    if (params->mass_len < a.src.cap || n_rows > a.dst.n_requests) return DS_ERR_ARG;
+    if ((uint64_t)n_rows * a.src.n_kv * (a.src.cap / 32 + 1) > kMaxGrid) return DS_ERR_SIZE;
+    a.mass_len = params->mass_len;
+    a.kept_len = params->kept_len;
+    a.n_rows = n_rows;
+    a.sinks = params->sinks;
+    a.recent = params->recent;
+    a.slack = params->slack;
+    evict_plan(a);
+    return DS_OK;
+}
+
 ds_status verify_args(const ds_verify_params *p, uint32_t n_rows, VerifyArgs &v)
 {
     if (!p) return DS_ERR_NULL;
@@ -146,46 +169,37 @@ ds_status ds_decode_attention(const ds_kv_cache *cache, const ds_decode_params *
     return run(ws, flags, s, [&](uint32_t *flag) { return flag ? decode_check(a, flag, s) : decode_launch(a, after_flag(ws), s); });
 }
 
+size_t ds_evict_workspace_bytes(const ds_kv_cache *src, const ds_kv_cache *dst, const ds_evict_params *params, uint32_t n_rows)
+{
+    EvictArgs a;
+    if (evict_args(src, dst, params, n_rows, a) != DS_OK) return 0;
+    return kFlagBytes + evict_ws_bytes(a);
+}
+
 ds_status ds_cache_evict(const ds_kv_cache *src, const ds_kv_cache *dst, const ds_evict_params *params, uint32_t n_rows,
                          const uint32_t *rows, const double *budget, const float *mass, float *mass_out, uint32_t *kept,
                          void *ws, size_t ws_bytes, uint32_t flags, ds_stream stream)
 {
-    if (!params) return DS_ERR_NULL;
-    EvictArgs a{};
-    ds_status st = view_of(src, params->max_len, a.src);
-    if (st == DS_OK) st = view_of(dst, 0, a.dst);
+    EvictArgs a;
+    ds_status st = evict_args(src, dst, params, n_rows, a);
     if (st != DS_OK) return st;
-    if (a.src.type != a.dst.type || a.src.page_size != a.dst.page_size || a.src.n_kv != a.dst.n_kv || a.src.dim != a.dst.dim ||
-        a.src.page_stride != a.dst.page_stride || a.src.token_stride != a.dst.token_stride ||
-        a.src.head_stride != a.dst.head_stride)
-        return DS_ERR_ARG;
-    if (params->mass_len < a.src.cap) return DS_ERR_ARG;
     if (n_rows == 0) return DS_OK;
-    if (n_rows > a.dst.n_requests || (!rows && n_rows > a.src.n_requests)) return DS_ERR_ARG;
-    if ((uint64_t)n_rows * a.src.n_kv * (a.src.cap / 32 + 1) > kMaxGrid) return DS_ERR_SIZE;
+    if (!rows && n_rows > a.src.n_requests) return DS_ERR_ARG;
     st = pointers_of(a.src);
     if (st == DS_OK) st = pointers_of(a.dst);
     if (st != DS_OK) return st;
     if (!budget || !mass || !mass_out || !kept) return DS_ERR_NULL;
     if (!aligned(budget, 8) || !aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(kept, 4) || !aligned(rows, 4))
         return DS_ERR_ALIGN;
-    if (flags & DS_VALIDATE) {
-        st = check_ws(ws, ws_bytes, kFlagBytes);
-        if (st != DS_OK) return st;
-    }
+    st = check_ws(ws, ws_bytes, kFlagBytes + evict_ws_bytes(a));
+    if (st != DS_OK) return st;
     a.rows = rows;
     a.budget = budget;
     a.mass = mass;
     a.mass_out = mass_out;
     a.kept = kept;
-    a.mass_len = params->mass_len;
-    a.kept_len = params->kept_len;
-    a.n_rows = n_rows;
-    a.sinks = params->sinks;
-    a.recent = params->recent;
-    a.slack = params->slack;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return run(ws, flags, s, [&](uint32_t *flag) { return flag ? evict_check(a, flag, s) : evict_launch(a, s); });
+    return run(ws, flags, s, [&](uint32_t *flag) { return flag ? evict_check(a, flag, s) : evict_launch(a, after_flag(ws), s); });
 }
 
 size_t ds_verify_workspace_bytes(const ds_verify_params *params, uint32_t n_rows)

@@ -116,8 +116,10 @@ def _load():
     lib.ds_cache_evict.argtypes = [P, P, P, u32, P, P, P, P, P, P, sz, u32, P]
     lib.ds_verify_draft.argtypes = [P, u32, P, P, P, P, P, P, P, P, P, P, P, P, sz, u32, P]
     lib.ds_decode_workspace_bytes.argtypes = [P, P, u32, i32]
+    lib.ds_evict_workspace_bytes.argtypes = [P, P, P, u32]
     lib.ds_verify_workspace_bytes.argtypes = [P, u32]
-    lib.ds_decode_workspace_bytes.restype = lib.ds_verify_workspace_bytes.restype = sz
+    for f in (lib.ds_decode_workspace_bytes, lib.ds_evict_workspace_bytes, lib.ds_verify_workspace_bytes):
+        f.restype = sz
     for f in (lib.ds_decode_attention, lib.ds_cache_evict, lib.ds_verify_draft):
         f.restype = i32
     for f in (lib.ds_characterize, lib.ds_characterize_score, lib.ds_characterize_score_noalloc,
@@ -726,11 +728,11 @@ def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0
     p_mass = _arg(mass, dev, torch.float32, _mass_shape(mass, cache), "mass")
     p_out = _arg(mass_out, dev, torch.float32, mass.shape, "mass_out")
     p_kept = _arg(kept, dev, torch.int32, None, "kept")
-    p = EvictParams(int(sinks), int(recent), int(slack), int(max_len), mass.shape[2], kept.shape[2])
-    if validate:
-        ws = _scratch(ws, 256, mass)
+    p = ctypes.byref(EvictParams(int(sinks), int(recent), int(slack), int(max_len), mass.shape[2], kept.shape[2]))
+    if n:
+        ws = _scratch(ws, lib.ds_evict_workspace_bytes(cache.ref, dst.ref, p, n), mass)
     p_ws = _arg(ws, dev, torch.uint8, None, "ws")
-    _check(lib.ds_cache_evict(cache.ref, dst.ref, ctypes.byref(p), n, p_rows, p_budget, p_mass, p_out, p_kept, p_ws,
+    _check(lib.ds_cache_evict(cache.ref, dst.ref, p, n, p_rows, p_budget, p_mass, p_out, p_kept, p_ws,
                               0 if ws is None else ws.numel(), _flags(validate), _stream_on(dev)))
     return dst.lens, kept
 

@@ -130,8 +130,8 @@ def evict(lens, budget, mass, rows, sinks, recent, slack, kept_len, dst_tokens):
             # NaN below every number, -inf among them
             worse = np.isnan(mass[r, h, :n])
             mid = np.arange(sinks, n - recent)
-            by = sorted(mid, key=lambda j: (worse[j], -m[j], j))[:keep - sinks - recent]
-            got[h] = np.concatenate([np.arange(sinks), np.sort(np.array(by, np.int64)), np.arange(n - recent, n)])
+            by = mid[np.lexsort((mid, -m[mid], worse[mid]))][:keep - sinks - recent]
+            got[h] = np.concatenate([np.arange(sinks), np.sort(by), np.arange(n - recent, n)])
         res.append(got)
     return res
 

@@ -415,6 +415,23 @@ def test_evict_long(ds):
     run_evict(ds, s, torch.tensor([17000.0, 29000.0], dtype=torch.float64), mass, [1, 0], 4, 100, inplace=True)
 
 
+@pytest.mark.parametrize("kind", ["spread", "equal", "few", "odd", "one bin", "late", "early"])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_evict_long_ties(ds, kind, inplace):
+    """Requests that are selected from in chunks: equal masses across chunks,
+    more masses of one first digit than are listed, short rows among long."""
+    lens = [20000, 24577, 8192, 8193, 1, 0, 40961]
+    s = Setup(ds, lens, 64, 2, 16, BF16, seed=27)
+    shape = (7, 2, 41000)
+    r = torch.rand(shape, generator=s.g)
+    mass = {"spread": (4 * torch.randn(shape, generator=s.g)).exp(), "equal": torch.full(shape, 0.25), "few": (r * 3).floor(),
+            "odd": torch.where(r < 0.2, float("nan"), torch.where(r < 0.4, float("inf"), torch.where(r < 0.6, -float("inf"), r))),
+            "one bin": 1.0 + r * 2.0 ** -3, "late": 1.0 + torch.arange(41000).expand(shape) * 2.0 ** -23,
+            "early": 1.0 - torch.arange(41000).expand(shape) * 2.0 ** -24}[kind].contiguous()
+    for share, sinks, recent in ((0.55, 4, 100), (0.01, 0, 0), (0.95, 9000, 9000), (0.0, 1, 0)):
+        run_evict(ds, s, s.lens.double() * share + 0.5, mass, [0, 6, 2, 5, 3, 4, 1], sinks, recent, inplace=inplace, max_len=40961)
+
+
 def test_evict_then_attend(ds):
     """Attention over the cut cache equals attention over the kept tokens."""
     s = Setup(ds, [600, 50], 16, 1, 64, BF16, seed=26)

@@ -29,8 +29,8 @@ def cache(ds, **kw):
 def test_exports_every_declared_symbol(ds):
     src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "driftsched_serve.h")).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(ds_[a-z_]+)\s*\(", src)))
-    assert names == ["ds_cache_evict", "ds_decode_attention", "ds_decode_workspace_bytes", "ds_verify_draft",
-                     "ds_verify_workspace_bytes"]
+    assert names == ["ds_cache_evict", "ds_decode_attention", "ds_decode_workspace_bytes", "ds_evict_workspace_bytes",
+                     "ds_verify_draft", "ds_verify_workspace_bytes"]
     for name in names:
         assert hasattr(ds.lib, name), name
 
@@ -103,7 +103,7 @@ def test_evict_needs_one_layout(ds, field, value):
 
 
 def test_evict_errors(ds):
-    def call(n=4, rows=FAKE, budget=FAKE, mass=FAKE, out=FAKE, kept=FAKE, flags=0, ws=None, ws_bytes=0, dst=None, **kw):
+    def call(n=4, rows=FAKE, budget=FAKE, mass=FAKE, out=FAKE, kept=FAKE, flags=0, ws=WS, ws_bytes=1 << 40, dst=None, **kw):
         p = ds.EvictParams(1, 1, 0, 0, 256, 256)
         for k, v in kw.items():
             setattr(p, k, v)
@@ -115,8 +115,21 @@ def test_evict_errors(ds):
     assert call(n=9, rows=None, dst=cache(ds, n_requests=20)) == ARG
     assert call(budget=None) == NULL and call(mass=None) == NULL and call(out=None) == NULL and call(kept=None) == NULL
     assert call(budget=0x1004) == ALIGN and call(kept=0x1002) == ALIGN and call(rows=0x1002) == ALIGN
-    assert call(flags=1) == WORKSPACE and call(flags=1, ws=WS, ws_bytes=255) == WORKSPACE
+    assert call(ws=None) == WORKSPACE and call(ws_bytes=255) == WORKSPACE and call(ws=0x100010) == WORKSPACE
     assert ds.lib.ds_cache_evict(ctypes.byref(cache(ds)), ctypes.byref(cache(ds)), None, 4, FAKE, FAKE, FAKE, FAKE, FAKE, None, 0, 0, None) == NULL
+
+
+def test_evict_workspace(ds):
+    """Nothing but the flag for short requests, chunks for long ones."""
+    p = ds.EvictParams(1, 1, 0, 0, 1 << 24, 1 << 24)
+    need = lambda c, n: ds.lib.ds_evict_workspace_bytes(ctypes.byref(c), ctypes.byref(c), ctypes.byref(p), n)   # noqa: E731
+    assert need(cache(ds, max_pages=1536), 4) == 256 and need(cache(ds, max_pages=1537), 4) > 256
+    assert need(cache(ds, max_pages=1 << 20), 4) > need(cache(ds, max_pages=4096), 4) > need(cache(ds, max_pages=4096), 2)
+    assert need(cache(ds, type=0), 4) == 0 and ds.lib.ds_evict_workspace_bytes(None, None, ctypes.byref(p), 4) == 0
+    big = cache(ds, max_pages=4096)
+    for ws_bytes, status in ((need(big, 4) - 1, WORKSPACE),):
+        assert ds.lib.ds_cache_evict(ctypes.byref(big), ctypes.byref(big), ctypes.byref(p), 4, FAKE, FAKE, FAKE, FAKE, FAKE, WS, ws_bytes, 0,
+                                     None) == status
 
 
 def test_verify_errors(ds):
