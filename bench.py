@@ -59,7 +59,7 @@ def parse():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--cpu-seconds", type=float, default=12.0)
     ap.add_argument("--stage", choices=["pipeline", "characterize", "errors", "drift", "simulate", "split",
-                                        "ceiling", "calibrate"],
+                                        "ceiling", "calibrate", "decode"],
                     default="pipeline",
                     help="characterize: time only stage 1 on --workload (any workload with text); "
                          "calibrate: stage 2 alone per call on the completion events of batch4k, "
@@ -70,7 +70,9 @@ def parse():
                          "the reference point of the paper's tokenizer-overhead table (no GPU); "
                          "errors: the estimation-error diagnostics on --workload's events; "
                          "drift: calibration at each alpha and the Aging re-sorts at every tick "
-                         "(drift4m); simulate: the dispatch-tick loop on --workload, per policy")
+                         "(drift4m); simulate: the dispatch-tick loop on --workload, per policy; "
+                         "decode: one decode step of the batch at the head of --workload's SJF order "
+                         "(attention over the paged cache, verification of drafts, eviction)")
     ap.add_argument("--settle", type=float, default=0.5,
                     help="seconds of untimed steps before the warmup steps (GPU clocks ramp "
                          "up under sustained load; the timed steps measure the steady state)")
@@ -221,6 +223,8 @@ def main():
         return bench_simulate(args, wl)
     if args.stage == "calibrate":
         return bench_calibrate(args)
+    if args.stage == "decode":
+        return bench_decode(args, wl)
     if not wl.has_text or len(wl.policies) < 5:
         print("bench.py: the step needs a workload with text and all five policies", file=sys.stderr)
         sys.exit(2)
@@ -608,6 +612,62 @@ def bench_calibrate(args):
                                   "us_per_call_graph": round(graph_ms * 1e3, 2),
                                   "GBs_graph": round(cal_bytes / (graph_ms * 1e-3) / 1e9, 1)}
     print(json.dumps(res))
+
+
+DECODE_BATCH, DECODE_DRAFTS = 32, 4
+
+
+def bench_decode(args, wl):
+    """One decode step of a dispatched batch: the requests at the head of the
+    workload's SJF order on the budgets of ds_score, each a third past its
+    budget; 4 drafted tokens per request, a bfloat16 cache of 8 key-value heads
+    of 128 dimensions for 32 query heads (one layer), pages of 64 tokens,
+    32,000 probabilities per position. Per call: attention with the weight per
+    cached token, verification, and the cut back to the budgets."""
+    import torch
+    from paper_2606_02982_amd import driftsched as ds
+    b = load(wl, with_text=False)
+    n, t, page, n_kv, n_q, dim, vocab = min(DECODE_BATCH, b.n), 1 + DECODE_DRAFTS, 64, 8, 32, 128, 32000
+    state = torch.ones(b.n_groups, dtype=torch.float64, device="cuda")
+    _, _, budget, _ = ds.score(to_dev(b.words), to_dev(b.category), to_dev(b.tenant), to_dev(b.group), to_dev(b.t_base),
+                               to_dev(b.s_tenant), state)
+    perm, _ = ds.order("sjf", to_dev(b.tier), to_dev(b.arrival), budget=budget, n_tiers=len(b.weights))
+    rows = perm[:n].contiguous()
+    budget = budget[rows.long()].contiguous()
+    lens = (budget * (4 / 3)).ceil().int()
+    most = int(lens.max())
+    per = -(-most // page)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    k, v = [torch.empty((2 * n * per, page, n_kv, dim), dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2)]
+    pages = torch.randperm(2 * n * per, generator=g, device="cuda").int().view(2, n, per)
+    cache = ds.kv_cache(k, v, pages[0].contiguous(), lens)
+    fresh = ds.kv_cache(k, v, pages[1].contiguous(), torch.zeros_like(lens))
+    mass = torch.zeros((n, n_kv, most), device="cuda")
+    q = torch.randn((n, t, n_q, dim), generator=g, device="cuda").bfloat16()
+    p = torch.softmax(4 * torch.randn((n, t, vocab), generator=g, device="cuda"), -1)
+    d = 0.8 * p[:, :-1] + 0.2 * torch.softmax(4 * torch.randn((n, t - 1, vocab), generator=g, device="cuda"), -1)
+    x = torch.multinomial(d.view(-1, vocab), 1, generator=g).view(n, t - 1).int()
+    u = torch.rand((n, t - 1), generator=g, device="cuda")
+    us = torch.rand(n, generator=g, device="cuda")
+    observed = torch.zeros(b.n, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    kept = torch.empty((n, n_kv, per * page), dtype=torch.int32, device="cuda")
+    cut_mass = torch.empty_like(mass)
+    attend = lambda: ds.decode_attention(q, cache, max_len=most, mass=mass, out=out)   # noqa: E731
+    verify = lambda: ds.verify_draft(p, d, x, u, us, rows=rows, observed=observed)   # noqa: E731
+    evict = lambda: ds.cache_evict(cache, fresh, budget, mass, sinks=4, recent=64, max_len=most, mass_out=cut_mass,   # noqa: E731
+                                   kept=kept)
+    ms = {"attention": timed_ms(attend, args), "verify": timed_ms(verify, args), "evict": timed_ms(evict, args)}
+    emitted = int(verify()[1].sum())
+    held = int(lens.sum())
+    step = ms["attention"] + ms["verify"]
+    print(json.dumps({"metric": "tokens emitted per second by a decode step (attention of one layer + verification)",
+                      "value": round(emitted / step * 1e3, 1), "unit": "tokens/s", "us": {c: round(1e3 * m, 1) for c, m in ms.items()},
+                      "attention_cache_GBs": round(held * n_kv * 2 * dim * 2 / ms["attention"] / 1e6, 1), "peak": HBM_PEAK_GBS,
+                      "emitted": emitted, "tokens_kept": int(fresh.lens.sum()), "steps": args.steps,
+                      "config": {"workload": wl.name, "batch": n, "cached_tokens": held, "drafts": DECODE_DRAFTS,
+                                 "query_heads": n_q, "kv_heads": n_kv, "head_dim": dim, "vocabulary": vocab}}), flush=True)
 
 
 def bench_drift(args, wl):

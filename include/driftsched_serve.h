@@ -41,6 +41,7 @@ typedef enum {
 #define DS_MAX_HEAD_DIM 256
 #define DS_MAX_NEW_TOKENS 16
 #define DS_MAX_QUERY_ROWS 1024   /* new tokens times query heads per key-value head */
+#define DS_MAX_MASS_TOKENS (1u << 24)   /* visible tokens of a request whose weights are gathered */
 #define DS_MAX_DRAFTS 63
 #define DS_MAX_VOCAB (1u << 24)
 
@@ -113,7 +114,7 @@ typedef struct {
  *       q_token_stride + h * q_head_stride + d; 16-byte aligned
  *  out  device, q_type, n_rows * n_tokens * n_q * head_dim; written
  *  mass device, float, or NULL. With mass a request may stand in one row only
- *       (DS_VALIDATE checks it)
+ *       (DS_VALIDATE checks it), and a query may see at most DS_MAX_MASS_TOKENS tokens (else DS_ERR_SIZE)
  *  ws   workspace of ds_decode_workspace_bytes(cache, params, n_rows, mass != NULL)
  */
 ds_status ds_decode_attention(const ds_kv_cache *cache, const ds_decode_params *params,

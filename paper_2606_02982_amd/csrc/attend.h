@@ -215,6 +215,8 @@ struct Attender {
     float scale;
     ScalarU32 table;
     const uint8_t *kh, *vh;
+    __amdgpu_buffer_rsrc_t score_rsrc;                         // this tile's rows of scores
+    uint32_t score_lane[kTiles];
     uint32_t k_lane, v_lane, token_bytes;                      // kFast: this lane's byte offsets
 
     uintx4 q[kTiles][kStepsK];
@@ -444,19 +446,17 @@ struct Attender {
                             for (int e = 0; e < 4; e++) s[t][2 * b + i][e] *= scale;
                 }
             }
-            if (a.scores) {
+            // without conditions, so that the loads under way are still
+            // counted behind it: rows past the last one, blocks past the
+            // split's end, and all of it where no weights are gathered, lie
+            // outside the buffer and are dropped
 #pragma unroll
-                for (int t = 0; t < kTiles; t++) {
-                    const uint32_t r = tile * 16 * kTiles + t * 16 + m;
-                    if (r < query_rows) {
-                        float *to = a.scores + (((uint64_t)row * a.c.n_kv + head) * query_rows + r) * a.score_len +
-                                    (uint64_t)v * kBlockTokens + g * 4;
+            for (int t = 0; t < kTiles; t++)
 #pragma unroll
-                        for (int i = 0; i < 2 * kSub; i++)
-                            if (v + i / 2 < v1) *reinterpret_cast<floatx4 *>(to + 16 * i) = s[t][i];
-                    }
-                }
-            }
+                for (int i = 0; i < 2 * kSub; i++)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uintx4, s[t][i]), score_rsrc,
+                                                           v + i / 2 < v1 ? score_lane[t] + 64 * i : 0xFFFFFFF0u,
+                                                           v * (kBlockTokens * 4), 0);
             // softmax step: s becomes the weights
             uintx4 p_hi[kTiles][kSub], p_lo[kTiles][kSub];
 #pragma unroll
@@ -634,6 +634,14 @@ void attend_kernel(const DecodeArgs a)
     w.token_bytes = (uint32_t)c.token_stride * A::kElem;
     w.k_lane = m * w.token_bytes + g * 16;
     w.v_lane = g * 4 * w.token_bytes + m * A::kVd * A::kElem;
+    {
+        const uint32_t rows = query_rows - tile * kRows < (uint32_t)kRows ? query_rows - tile * kRows : kRows;
+        const uint64_t first = (((uint64_t)row * c.n_kv + head) * query_rows + tile * kRows) * a.score_len;
+        w.score_rsrc = __builtin_amdgcn_make_buffer_rsrc(a.scores + (a.scores ? first : 0), 0,
+                                                         a.scores ? (int)(rows * a.score_len * 4) : 0, 0x00027000);
+#pragma unroll
+        for (int t = 0; t < kTiles; t++) w.score_lane[t] = ((t * 16 + m) * a.score_len + g * 4) * 4;
+    }
     // this lane's queries (one column of each tile)
 #pragma unroll
     for (int t = 0; t < kTiles; t++) {

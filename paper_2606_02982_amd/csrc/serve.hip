@@ -142,6 +142,7 @@ size_t ds_decode_workspace_bytes(const ds_kv_cache *cache, const ds_decode_param
 {
     DecodeArgs a;
     if (decode_args(cache, params, n_rows, a) != DS_OK) return 0;
+    if (n_rows && with_mass && a.score_len > DS_MAX_MASS_TOKENS) return 0;
     return kFlagBytes + (n_rows ? decode_ws_bytes(a, with_mass != 0) : 0);
 }
 
@@ -154,6 +155,7 @@ ds_status ds_decode_attention(const ds_kv_cache *cache, const ds_decode_params *
     if (st != DS_OK) return st;
     if (mass && a.mass_len < a.c.cap) return DS_ERR_ARG;
     if (n_rows == 0) return DS_OK;
+    if (mass && a.score_len > DS_MAX_MASS_TOKENS) return DS_ERR_SIZE;
     if (!rows && n_rows > a.c.n_requests) return DS_ERR_ARG;
     st = pointers_of(a.c);
     if (st != DS_OK) return st;
