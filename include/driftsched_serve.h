@@ -19,7 +19,9 @@
  * point" holds here too: device arrays, host parameter structs, workspaces of
  * the caller, enqueueing on the caller's stream, status codes, DS_VALIDATE.
  * `rows` names the batch: rows[i] is the request of row i, e.g. the first
- * n_rows entries of a ds_order permutation; NULL: row i is request i.
+ * n_rows entries of a ds_order permutation; NULL: row i is request i. A
+ * workspace of 256 bytes is used by DS_VALIDATE only and may be NULL without
+ * that flag.
  */
 #ifndef DRIFTSCHED_SERVE_H
 #define DRIFTSCHED_SERVE_H

@@ -34,7 +34,7 @@ ds_status run(void *ws, uint32_t flags, hipStream_t s, F &&enqueue)
     return hip_status(enqueue(nullptr));
 }
 
-inline void *after_flag(void *ws) { return static_cast<uint8_t *>(ws) + kFlagBytes; }
+inline void *after_flag(void *ws) { return ws ? static_cast<uint8_t *>(ws) + kFlagBytes : nullptr; }
 
 // The integer a C caller passed for an enum-typed argument. C allows any int
 // there; in C++ a value outside the enumeration's range may not be read as

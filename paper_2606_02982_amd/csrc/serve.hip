@@ -115,6 +115,12 @@ ds_status evict_args(const ds_kv_cache *src, const ds_kv_cache *dst, const ds_ev
     return DS_OK;
 }
 
+// A workspace of the flag alone is used by DS_VALIDATE only.
+ds_status check_scratch(void *ws, size_t ws_bytes, size_t need, uint32_t flags)
+{
+    return need || (flags & DS_VALIDATE) ? check_ws(ws, ws_bytes, kFlagBytes + need) : DS_OK;
+}
+
 ds_status verify_args(const ds_verify_params *p, uint32_t n_rows, VerifyArgs &v)
 {
     if (!p) return DS_ERR_NULL;
@@ -161,7 +167,7 @@ ds_status ds_decode_attention(const ds_kv_cache *cache, const ds_decode_params *
     if (st != DS_OK) return st;
     if (!q || !out) return DS_ERR_NULL;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(rows, 4) || !aligned(mass, 4)) return DS_ERR_ALIGN;
-    st = check_ws(ws, ws_bytes, kFlagBytes + decode_ws_bytes(a, mass != nullptr));
+    st = check_scratch(ws, ws_bytes, decode_ws_bytes(a, mass != nullptr), flags);
     if (st != DS_OK) return st;
     a.rows = rows;
     a.q = q;
@@ -193,7 +199,7 @@ ds_status ds_cache_evict(const ds_kv_cache *src, const ds_kv_cache *dst, const d
     if (!budget || !mass || !mass_out || !kept) return DS_ERR_NULL;
     if (!aligned(budget, 8) || !aligned(mass, 4) || !aligned(mass_out, 4) || !aligned(kept, 4) || !aligned(rows, 4))
         return DS_ERR_ALIGN;
-    st = check_ws(ws, ws_bytes, kFlagBytes + evict_ws_bytes(a));
+    st = check_scratch(ws, ws_bytes, evict_ws_bytes(a), flags);
     if (st != DS_OK) return st;
     a.rows = rows;
     a.budget = budget;

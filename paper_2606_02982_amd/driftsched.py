@@ -605,11 +605,17 @@ def _arg(t, index, dtype, shape, name):
     return t.data_ptr()
 
 
-def _scratch(ws, need, like):
-    """The caller's workspace, or one of this call alone: taken from torch's
-    allocator on the current stream, so calls on other streams and in captured
-    graphs share nothing with it."""
-    return like.new_empty(max(need, 256), dtype=torch.uint8) if ws is None else ws
+def _scratch(ws, need, like, index, validate):
+    """Address and size of the workspace, and what holds it: the caller's, or
+    one of this call alone, taken from torch's allocator on the current stream,
+    so that calls on other streams and in captured graphs share nothing with
+    it; none where the call has no use for it."""
+    if ws is None:
+        if need <= 256 and not validate:
+            return None, 0, None
+        ws = like.new_empty(max(need, 256), dtype=torch.uint8)
+        return ws.data_ptr(), max(need, 256), ws
+    return _arg(ws, index, torch.uint8, None, "ws"), ws.numel(), ws
 
 
 class Cache:
@@ -686,19 +692,19 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
     if dev != cache.index:
         raise ValueError("q and the cache must be on one device")
     n, t, h, d = shape = q.shape
+    p_rows = _arg(rows, dev, torch.int32, shape[:1], "rows")
     if out is None:
         out = q.new_empty(shape)
-    p_rows = _arg(rows, dev, torch.int32, shape[:1], "rows")
-    p_out = _arg(out, dev, q.dtype, shape, "out")
+        p_out = out.data_ptr()
+    else:
+        p_out = _arg(out, dev, q.dtype, shape, "out")
     p_mass = None if mass is None else _arg(mass, dev, torch.float32, _mass_shape(mass, cache), "mass")
     s_row, s_token, s_head, _ = q.stride()
     p = ctypes.byref(DecodeParams(h, t, DTYPES[q.dtype], s_row, s_token, s_head, d ** -0.5 if scale is None else float(scale),
                                   int(window), int(sinks), int(max_len), 0 if mass is None else mass.shape[2]))
-    if n:
-        ws = _scratch(ws, lib.ds_decode_workspace_bytes(cache.ref, p, n, mass is not None), q)
-    p_ws = _arg(ws, dev, torch.uint8, None, "ws")
-    _check(lib.ds_decode_attention(cache.ref, p, n, p_rows, q.data_ptr(), p_out, p_mass, p_ws, 0 if ws is None else ws.numel(),
-                                   _flags(validate), _stream_on(dev)))
+    p_ws, ws_bytes, ws = _scratch(ws, lib.ds_decode_workspace_bytes(cache.ref, p, n, mass is not None), q, dev, validate)
+    _check(lib.ds_decode_attention(cache.ref, p, n, p_rows, q.data_ptr(), p_out, p_mass, p_ws, ws_bytes, _flags(validate),
+                                   _stream_on(dev)))
     return out
 
 
@@ -729,11 +735,9 @@ def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0
     p_out = _arg(mass_out, dev, torch.float32, mass.shape, "mass_out")
     p_kept = _arg(kept, dev, torch.int32, None, "kept")
     p = ctypes.byref(EvictParams(int(sinks), int(recent), int(slack), int(max_len), mass.shape[2], kept.shape[2]))
-    if n:
-        ws = _scratch(ws, lib.ds_evict_workspace_bytes(cache.ref, dst.ref, p, n), mass)
-    p_ws = _arg(ws, dev, torch.uint8, None, "ws")
-    _check(lib.ds_cache_evict(cache.ref, dst.ref, p, n, p_rows, p_budget, p_mass, p_out, p_kept, p_ws,
-                              0 if ws is None else ws.numel(), _flags(validate), _stream_on(dev)))
+    p_ws, ws_bytes, ws = _scratch(ws, lib.ds_evict_workspace_bytes(cache.ref, dst.ref, p, n), mass, dev, validate)
+    _check(lib.ds_cache_evict(cache.ref, dst.ref, p, n, p_rows, p_budget, p_mass, p_out, p_kept, p_ws, ws_bytes,
+                              _flags(validate), _stream_on(dev)))
     return dst.lens, kept
 
 
@@ -765,10 +769,6 @@ def verify_draft(target, draft, tokens, u, u_sample, n_draft=None, rows=None, ob
     dev, i32, f32 = _device_of(target), torch.int32, torch.float32
     if draft is not None and draft.get_device() != dev:
         raise ValueError("draft must be on the target's device")
-    if out is None:
-        out = target.new_empty((n, k + 1), dtype=i32)
-    if n_emitted is None:
-        n_emitted = target.new_empty(n, dtype=i32)
     at = lens if observed is None else observed
     n_req = n if at is None else at.numel()
     p_tokens = _arg(tokens, dev, i32, (n, k), "tokens")
@@ -778,15 +778,21 @@ def verify_draft(target, draft, tokens, u, u_sample, n_draft=None, rows=None, ob
     p_rows = _arg(rows, dev, i32, (n,), "rows")
     p_observed = _arg(observed, dev, i32, (n_req,), "observed")
     p_lens = _arg(lens, dev, i32, (n_req,), "lens")
-    p_out = _arg(out, dev, i32, (n, k + 1), "out")
-    p_emitted = _arg(n_emitted, dev, i32, (n,), "n_emitted")
+    if out is None:
+        out = target.new_empty((n, k + 1), dtype=i32)
+        p_out = out.data_ptr()
+    else:
+        p_out = _arg(out, dev, i32, (n, k + 1), "out")
+    if n_emitted is None:
+        n_emitted = target.new_empty(n, dtype=i32)
+        p_emitted = n_emitted.data_ptr()
+    else:
+        p_emitted = _arg(n_emitted, dev, i32, (n,), "n_emitted")
     t_row, t_pos, _ = target.stride()
     d_row, d_pos, _ = (0, 0, 0) if draft is None else draft.stride()
     p = ctypes.byref(VerifyParams(k, vocab, n_req, kind, t_row, t_pos, d_row, d_pos))
-    if n:
-        ws = _scratch(ws, lib.ds_verify_workspace_bytes(p, n), target)
-    p_ws = _arg(ws, dev, torch.uint8, None, "ws")
+    p_ws, ws_bytes, ws = _scratch(ws, lib.ds_verify_workspace_bytes(p, n), target, dev, validate)
     _check(lib.ds_verify_draft(p, n, p_rows, target.data_ptr(), None if draft is None else draft.data_ptr(), p_tokens, p_draft,
-                               p_u, p_sample, p_out, p_emitted, p_observed, p_lens, p_ws, 0 if ws is None else ws.numel(),
-                               _flags(validate), _stream_on(dev)))
+                               p_u, p_sample, p_out, p_emitted, p_observed, p_lens, p_ws, ws_bytes, _flags(validate),
+                               _stream_on(dev)))
     return out, n_emitted

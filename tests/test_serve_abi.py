@@ -66,7 +66,8 @@ def test_cache_errors(ds, field, value, status):
     (dict(n_q=2 * 1025), SIZE), (dict(n_q=2 * 512, n_tokens=3), SIZE), (dict(mass=FAKE, mass_len=255), ARG),
     (dict(n_rows=9, rows=None), ARG), (dict(n_rows=0xFFFFFFFF), SIZE), (dict(q=None), NULL), (dict(out=None), NULL),
     (dict(q=0x1008), ALIGN), (dict(out=0x1002), ALIGN), (dict(rows=0x1001), ALIGN), (dict(mass=0x1002), ALIGN),
-    (dict(ws=None), WORKSPACE), (dict(ws=0x100010), WORKSPACE), (dict(ws_bytes=255), WORKSPACE), (dict(n_rows=0), OK)])
+    (dict(ws=None, flags=1), WORKSPACE), (dict(ws=0x100010, flags=1), WORKSPACE), (dict(ws_bytes=255, flags=1), WORKSPACE),
+    (dict(mass=FAKE, ws=None), WORKSPACE), (dict(n_rows=0), OK)])
 def test_decode_errors(ds, kw, status):
     assert decode(ds, **kw) == status
 
@@ -115,7 +116,7 @@ def test_evict_errors(ds):
     assert call(n=9, rows=None, dst=cache(ds, n_requests=20)) == ARG
     assert call(budget=None) == NULL and call(mass=None) == NULL and call(out=None) == NULL and call(kept=None) == NULL
     assert call(budget=0x1004) == ALIGN and call(kept=0x1002) == ALIGN and call(rows=0x1002) == ALIGN
-    assert call(ws=None) == WORKSPACE and call(ws_bytes=255) == WORKSPACE and call(ws=0x100010) == WORKSPACE
+    assert call(flags=1, ws=None) == WORKSPACE and call(flags=1, ws_bytes=255) == WORKSPACE and call(flags=1, ws=0x100010) == WORKSPACE
     assert ds.lib.ds_cache_evict(ctypes.byref(cache(ds)), ctypes.byref(cache(ds)), None, 4, FAKE, FAKE, FAKE, FAKE, FAKE, None, 0, 0, None) == NULL
 
 
