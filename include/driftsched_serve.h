@@ -66,7 +66,9 @@ typedef enum {
  *  type       DS_F16, DS_BF16 or DS_E4M3
  * n_requests, max_pages, n_pages, page_size, n_kv >= 1; max_pages * page_size
  * <= DS_MAX_ITEMS.
- * Tokens whose page is out of range are taken as absent.
+ * Tokens whose page is out of range are taken as absent. Pages are memory as a
+ * whole: every slot of a page that holds a token may be read, and those of
+ * page 0.
  */
 typedef struct {
     void *k, *v;

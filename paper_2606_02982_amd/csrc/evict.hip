@@ -65,6 +65,7 @@ constexpr int kCopyPitch = kBins + 16;     // the copies of a bin lie in differe
 // 32,768 48 / 179 and 44 / 176, 100,000 139 / 564 and 98 / 537 us).
 constexpr uint32_t kLongTokens = 24576;
 constexpr uint32_t kMaxChunks = 256;
+constexpr uint32_t kCopyGroups = 1u << 23; // workgroups of a copy, where there are no more (row, head)
 constexpr int kAhead = 8;                  // groups of 64 tokens under way per wave
 constexpr uint32_t kList = 8192;           // masses with the first digit sought that fit into LDS
 struct Select {
@@ -534,31 +535,33 @@ __device__ __forceinline__ void put(uint8_t *to, const uint8_t *from)
     __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const uintx4 *>(from)), reinterpret_cast<uintx4 *>(to));
 }
 
-// 16 bytes of a key or value per thread and step.
-__global__ __launch_bounds__(256) void copy_kernel(const EvictArgs a, uint32_t chunks, uint32_t tokens, uint32_t elem)
+// 16 bytes of a key or value per thread and step; `groups` workgroups share a
+// (row, head) in pieces of `tokens` kept tokens.
+__global__ __launch_bounds__(256) void copy_kernel(const EvictArgs a, uint32_t groups, uint32_t tokens, uint32_t elem)
 {
-    const uint32_t chunk = blockIdx.x % chunks, head = blockIdx.x / chunks % a.src.n_kv;
-    const uint32_t row = blockIdx.x / chunks / a.src.n_kv;
+    const uint32_t pair = blockIdx.x / groups, head = pair % a.src.n_kv, row = pair / a.src.n_kv;
     const Cut x = cut_of(a, row);
-    if (x.keep == x.n || chunk * tokens >= x.keep) return;
+    if (x.keep == x.n) return;
     const KvView &s = a.src, &d = a.dst;
-    const uint32_t *kept = a.kept + ((uint64_t)row * s.n_kv + head) * a.kept_len;
-    const uint32_t left = x.keep - chunk * tokens, count = left < tokens ? left : tokens;
-    if (a.n_chunks && threadIdx.x < count) {
-        // the chunks' walks may not write into masses that others still read
-        const uint32_t to = chunk * tokens + threadIdx.x;
-        a.mass_out[((uint64_t)x.req * s.n_kv + head) * a.mass_len + to] = a.kept_mass[((uint64_t)row * s.n_kv + head) * a.most_kept + to];
-    }
+    const uint32_t *kept = a.kept + (uint64_t)pair * a.kept_len;
     const uint32_t units = s.dim * elem / 16;
-    for (uint32_t i = threadIdx.x; i < count * units; i += 256) {
-        const uint32_t to = chunk * tokens + i / units, from = kept[to], u = i % units;
-        const uint32_t sp = s.table[(uint64_t)x.req * s.max_pages + from / s.page_size];
-        const uint32_t dp = d.table[(uint64_t)row * d.max_pages + to / d.page_size];
-        if (sp >= s.n_pages || dp >= d.n_pages) continue;
-        const uint64_t sa = (sp * s.page_stride + (from % s.page_size) * s.token_stride + head * s.head_stride) * elem + u * 16;
-        const uint64_t da = (dp * d.page_stride + (to % d.page_size) * d.token_stride + head * d.head_stride) * elem + u * 16;
-        put(d.k + da, s.k + sa);
-        put(d.v + da, s.v + sa);
+    for (uint32_t first = blockIdx.x % groups * tokens; first < x.keep; first += groups * tokens) {
+        const uint32_t left = x.keep - first, count = left < tokens ? left : tokens;
+        if (a.n_chunks && threadIdx.x < count) {
+            // the chunks' walks may not write into masses that others still read
+            const uint32_t to = first + threadIdx.x;
+            a.mass_out[((uint64_t)x.req * s.n_kv + head) * a.mass_len + to] = a.kept_mass[(uint64_t)pair * a.most_kept + to];
+        }
+        for (uint32_t i = threadIdx.x; i < count * units; i += 256) {
+            const uint32_t to = first + i / units, from = kept[to], u = i % units;
+            const uint32_t sp = s.table[(uint64_t)x.req * s.max_pages + from / s.page_size];
+            const uint32_t dp = d.table[(uint64_t)row * d.max_pages + to / d.page_size];
+            if (sp >= s.n_pages || dp >= d.n_pages) continue;
+            const uint64_t sa = (sp * s.page_stride + (from % s.page_size) * s.token_stride + head * s.head_stride) * elem + u * 16;
+            const uint64_t da = (dp * d.page_stride + (to % d.page_size) * d.token_stride + head * d.head_stride) * elem + u * 16;
+            put(d.k + da, s.k + sa);
+            put(d.v + da, s.v + sa);
+        }
     }
 }
 
@@ -616,7 +619,8 @@ hipError_t evict_launch(EvictArgs a, void *ws, hipStream_t s)
     const uint32_t tokens = bytes >= 256 ? 32 : bytes <= 32 ? 256 : 8192 / bytes;
     const uint32_t chunks = (uint32_t)cdiv(a.most_kept, tokens);
     if (!chunks) return hipSuccess;
-    copy_kernel<<<pairs * chunks, 256, 0, s>>>(a, chunks, tokens, elem);
+    const uint32_t share = kCopyGroups / pairs ? kCopyGroups / pairs : 1, groups = chunks < share ? chunks : share;
+    copy_kernel<<<pairs * groups, 256, 0, s>>>(a, groups, tokens, elem);
     return hipGetLastError();
 }
 

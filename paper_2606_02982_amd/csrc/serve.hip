@@ -9,7 +9,8 @@ using namespace ds;
 
 namespace {
 
-constexpr uint64_t kMaxGrid = 0x7FFFFFFFull;
+// workgroups of a launch: its threads are counted in 32 bits
+constexpr uint64_t kMaxGrid = 0xFFFFFFFFull / 256, kMaxGrid1024 = 0xFFFFFFFFull / 1024;
 constexpr uint32_t kMaxTokens = DS_MAX_ITEMS;   // of a request; windows and sinks beyond act like it
 
 uint32_t clamp32(uint32_t x, uint32_t most) { return x < most ? x : most; }
@@ -104,7 +105,6 @@ ds_status evict_args(const ds_kv_cache *src, const ds_kv_cache *dst, const ds_ev
         a.src.head_stride != a.dst.head_stride)
         return DS_ERR_ARG;
     if (params->mass_len < a.src.cap || n_rows > a.dst.n_requests) return DS_ERR_ARG;
-    if ((uint64_t)n_rows * a.src.n_kv * (a.src.cap / 32 + 1) > kMaxGrid) return DS_ERR_SIZE;
     a.mass_len = params->mass_len;
     a.kept_len = params->kept_len;
     a.n_rows = n_rows;
@@ -112,6 +112,7 @@ ds_status evict_args(const ds_kv_cache *src, const ds_kv_cache *dst, const ds_ev
     a.recent = params->recent;
     a.slack = params->slack;
     evict_plan(a);
+    if ((uint64_t)n_rows * a.src.n_kv * (a.n_chunks ? a.n_chunks : 1) > kMaxGrid1024) return DS_ERR_SIZE;
     return DS_OK;
 }
 

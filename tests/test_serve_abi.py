@@ -87,6 +87,13 @@ def test_decode_workspace(ds):
     for m in (None, FAKE):
         need = f(4, m is not None)
         assert ds.lib.ds_decode_attention(ctypes.byref(c), ctypes.byref(p), 4, FAKE, FAKE, FAKE, m, WS, need - 1, 0, None) == WORKSPACE
+    # weights of more than 2^24 tokens are not gathered; with a window they need not be
+    huge, p = cache(ds, max_pages=(1 << 20) + 16), ds.DecodeParams(8, 2, 2, 1024, 512, 64, 0.125, 0, 0, 0, 1 << 26)
+    g = lambda m: ds.lib.ds_decode_workspace_bytes(ctypes.byref(huge), ctypes.byref(p), 1, m)   # noqa: E731
+    assert g(0) > 256 and g(1) == 0
+    assert ds.lib.ds_decode_attention(ctypes.byref(huge), ctypes.byref(p), 1, FAKE, FAKE, FAKE, FAKE, WS, 1 << 50, 0, None) == SIZE
+    p.window = 4096
+    assert g(1) > 256
     # 8-bit caches go with either query type
     for t in (1, 2):
         q = ds.DecodeParams(8, 1, t, 512, 512, 64, 0.125, 0, 0, 0, 0)
@@ -112,6 +119,8 @@ def test_evict_errors(ds):
                                      ws, ws_bytes, flags, None)
     assert call(n=0) == OK
     assert call(n=9) == ARG                                    # more rows than dst holds
+    assert ds.lib.ds_evict_workspace_bytes(*map(ctypes.byref, (cache(ds, n_requests=1 << 28),) * 2 + (ds.EvictParams(1, 1, 0, 0, 256, 256),)),
+                                           1 << 28) == 0       # more workgroups than a launch takes
     assert call(mass_len=255) == ARG and call(max_len=300) == ARG
     assert call(n=9, rows=None, dst=cache(ds, n_requests=20)) == ARG
     assert call(budget=None) == NULL and call(mass=None) == NULL and call(out=None) == NULL and call(kept=None) == NULL
