@@ -146,6 +146,50 @@ def test_attention_long(ds, n_rows, length, dim, group, t):
     s.attend(ds, queries(s, n_rows, t, group, dim, BF16), mass=torch.rand((n_rows, 1, length), generator=s.g), max_len=length)
 
 
+@pytest.mark.parametrize("n_rows", [257, 1024, 1025, 1500])
+def test_attention_many_rows(ds, n_rows):
+    """Several lengths per thread that looks for slots; so many rows that
+    every row is one slot."""
+    g = torch.Generator().manual_seed(n_rows)
+    lens = torch.randint(0, 400, (n_rows,), generator=g)
+    lens[::7] = torch.randint(0, 3, lens[::7].shape, generator=g)
+    lens[n_rows // 2] = 2900
+    s = Setup(ds, lens.tolist(), 16, 1, 64, BF16, seed=n_rows)
+    rows = torch.randperm(n_rows, generator=g).to(torch.int32)
+    s.attend(ds, queries(s, n_rows, 1, 2, 64, BF16), rows=rows, mass=torch.rand((n_rows, 1, 2900), generator=g), max_len=2900)
+
+
+@pytest.mark.parametrize("n_kv,dim,kt", [(3, 128, BF16), (9, 128, F16), (16, 128, BF16), (5, 64, BF16), (3, 64, E4M3), (16, 128, E4M3), (4, 256, BF16)])
+def test_attention_orders(ds, n_kv, dim, kt):
+    """Each order in which workgroups take slots and heads, rows in several slots."""
+    lens = [3000, 0, 1777, 40, 2500]
+    s = Setup(ds, lens, 32, n_kv, dim, kt, seed=n_kv)
+    qt = BF16 if kt == E4M3 else kt
+    s.attend(ds, queries(s, 5, 2, 2 * n_kv, dim, qt), mass=torch.rand((5, n_kv, 3008), generator=s.g))
+    s.attend(ds, queries(s, 5, 5, 8 * n_kv, dim, qt), window=1500, sinks=40)
+
+
+def test_attention_broadcast_queries(ds):
+    """One row of queries for every request (stride 0)."""
+    s = Setup(ds, LENS, 16, 2, 64, BF16, seed=12)
+    q = queries(s, 1, 2, 4, 64, BF16)
+    out = ds.decode_attention(q.cuda().expand(len(LENS), 2, 4, 64), s.cache, validate=True)
+    want, off, _, _ = ref.attention(q.expand(len(LENS), 2, 4, 64), s.k, s.v, s.table, s.lens)
+    ref.check_out(out.cpu(), want, off, BF16)
+
+
+def test_shared_pages(ds):
+    """Two requests with a common prefix: each has masses of its own, and what
+    one loses by an eviction the other keeps."""
+    s = Setup(ds, [200, 300, 250], 16, 2, 64, BF16, seed=13)
+    s.table[1, :9] = s.table[0, :9]
+    s.push()
+    mass = torch.rand((3, 2, 304), generator=s.g)
+    s.attend(ds, queries(s, 3, 1, 4, 64, BF16), mass=mass)
+    want = run_evict(ds, s, torch.tensor([90.0, 120.0, 300.0], dtype=torch.float64), mass, [0, 1, 2], 4, 16, one_pool=True)
+    assert [w is not None for w in want] == [True, True, False]
+
+
 def test_attention_large_scores(ds):
     """Scores of some hundreds: one token takes nearly all the weight."""
     s = Setup(ds, LENS, 16, 2, 64, BF16, seed=3)
@@ -624,6 +668,39 @@ def test_step_in_a_graph(ds):
         for x, y in zip(state_of(a), state_of(b)):
             assert torch.equal(x, y), i
         del junk
+
+
+def test_two_graphs_side_by_side(ds):
+    """Two captured steps replayed at once on two streams."""
+    alone, graphs, state = [], [], []
+    for seed in (43, 44):
+        a = step_inputs(ds, seed)
+        for _ in range(4):
+            r = decode_step(ds, **a)
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in r] + state_of(a))
+        b = step_inputs(ds, seed)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            decode_step(ds, **b)                          # the first of the four
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = decode_step(ds, **b)
+        graphs.append(graph)
+        state.append((b, got))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(3):
+        for stream, graph in zip(streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (b, got), want in zip(state, alone):
+        for x, y in zip(list(got) + state_of(b), want):
+            assert torch.equal(x, y)
 
 
 def test_steps_on_two_streams(ds):
