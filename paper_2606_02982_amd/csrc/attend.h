@@ -280,8 +280,9 @@ struct Attender {
 
     // kStream: whole cache lines that no other workgroup reads go past the
     // caches (16 heads of 128 dimensions in 16 bits: 380 -> 370 us for 2.1 GB,
-    // 8 heads of 256: 348 -> 336 us; in 8 bits 217 -> 222 us, two tiles of
-    // query rows 268 -> 365 us).
+    // 8 heads of 256: 348 -> 336 us, 20 query rows 216 -> 199 us; in 8 bits
+    // 217 -> 222 us, 40 query rows, whose two units read the same, 268 -> 365
+    // us).
     template <typename W>
     static __device__ __forceinline__ W fetch(const uint8_t *p)
     {
@@ -737,7 +738,8 @@ hipError_t attend(const DecodeArgs &a, hipStream_t s)
 {
     const uint32_t dim = padded_dim(a.c.dim), tiles = unit_tiles(a.c.dim, a.group * a.tokens);
     if (dim == 64) return tiles == 1 ? attend_page<T, kE4m3, 64, 1, false>(a, s) : attend_page<T, kE4m3, 64, 2, false>(a, s);
-    if (dim == 128) return tiles == 1 ? attend_page<T, kE4m3, 128, 1, !kE4m3>(a, s) : attend_page<T, kE4m3, 128, 2, false>(a, s);
+    if (dim == 128 && tiles == 1) return attend_page<T, kE4m3, 128, 1, !kE4m3>(a, s);
+    if (dim == 128) return a.n_tiles == 1 ? attend_page<T, kE4m3, 128, 2, !kE4m3>(a, s) : attend_page<T, kE4m3, 128, 2, false>(a, s);
     if constexpr (!kE4m3)
         if (a.n_tiles == 1) return attend_page<T, kE4m3, 256, 1, true>(a, s);
     return attend_page<T, kE4m3, 256, 1, false>(a, s);
