@@ -30,6 +30,9 @@
  *
  *   ds_read_bandwidth   the read side of ds_characterize alone
  *
+ * The decode step of the batch that the order dispatches is in
+ * driftsched_serve.h.
+ *
  * Conventions shared by every entry point:
  *  - Array arguments are DEVICE pointers (memory from hipMalloc or any
  *    allocator of the same device, e.g. torch tensors); parameter structs

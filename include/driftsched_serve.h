@@ -116,7 +116,7 @@ typedef struct {
  *
  *  q    device, q_type, element (i, t, h, d) at i * q_row_stride + t *
  *       q_token_stride + h * q_head_stride + d; 16-byte aligned
- *  out  device, q_type, n_rows * n_tokens * n_q * head_dim; written
+ *  out  device, q_type, n_rows * n_tokens * n_q * head_dim; written, and apart from q
  *  mass device, float, or NULL. With mass a request may stand in one row only
  *       (DS_VALIDATE checks it), and a query may see at most DS_MAX_MASS_TOKENS tokens (else DS_ERR_SIZE)
  *  ws   workspace of ds_decode_workspace_bytes(cache, params, n_rows, mass != NULL)
@@ -158,7 +158,7 @@ typedef struct {
  *             request per row (dst->n_requests >= n_rows) and len is written
  *  budget     device, n_requests double, e.g. from ds_score; NaN: not cut
  *  mass       device, n_requests * n_kv * mass_len float, as ds_decode_attention leaves it
- *  mass_out   device, like mass, may be mass itself: its entries 0 .. keep-1
+ *  mass_out   device, like mass, mass itself or apart from it: its entries 0 .. keep-1
  *             receive the kept tokens' masses for the requests that are cut;
  *             nothing else is written
  *  kept       device, n_rows * n_kv * kept_len uint32: entries 0 .. keep-1 of

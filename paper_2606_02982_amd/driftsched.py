@@ -683,7 +683,8 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
     and first tokens always seen. ``max_len``: the most tokens any request of
     the batch holds, if known (a tighter launch and workspace). ``mass``:
     float32 (n_requests, n_kv, length >= max_len), updated in place with the
-    weight each cached token received. Returns out, shaped like q."""
+    weight each cached token received. ``out`` must not overlap q. Returns out,
+    shaped like q."""
     if q.dim() != 4 or q.shape[3] != cache.head_dim or q.stride(3) != 1:
         raise ValueError("q must be (n_rows, n_tokens, n_q, head_dim) with a dense last axis")
     if q.dtype is not torch.bfloat16 and q.dtype is not torch.float16:

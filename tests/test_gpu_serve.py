@@ -178,6 +178,20 @@ def test_attention_broadcast_queries(ds):
     ref.check_out(out.cpu(), want, off, BF16)
 
 
+def test_no_rows(ds):
+    """An empty batch: nothing is read or written."""
+    s = Setup(ds, [5, 40], 16, 2, 64, BF16, seed=14)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    mass = torch.ones((2, 2, 48), device="cuda")
+    out = ds.decode_attention(torch.zeros((0, 2, 4, 64), dtype=BF16, device="cuda"), s.cache, rows=none, mass=mass)
+    assert out.shape == (0, 2, 4, 64)
+    left, kept = ds.cache_evict(s.cache, s.cache, torch.zeros(2, dtype=torch.float64, device="cuda"), mass, rows=none)
+    assert kept.shape[0] == 0 and left.tolist() == [5, 40] and (mass == 1).all()
+    p, q, x, u, us, g = drafted(2, 3, 100, F32, 81)
+    out, emitted = ds.verify_draft(p[:0].cuda(), q[:0].cuda(), x[:0].cuda(), u[:0].cuda(), us[:0].cuda())
+    assert out.shape == (0, 4) and emitted.numel() == 0
+
+
 def test_shared_pages(ds):
     """Two requests with a common prefix: each has masses of its own, and what
     one loses by an eviction the other keeps."""
