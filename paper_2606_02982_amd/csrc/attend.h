@@ -178,10 +178,13 @@ __device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
 
 // One wave's share of a unit: steps wave, wave + 4, ... of the slot's blocks
 // (see DecodeArgs for slots and units).
-// kDim: padded dimensions; kTiles: 16-row tiles of queries; kFast: all kDim
-// dimensions are there and a page holds a multiple of 16 tokens, so half a
-// block lies in one page, its address is the same for the whole wave, and a
-// lane's place in it is a 32-bit offset. Otherwise addresses are per lane.
+// kDim: padded dimensions; kTiles: 16-row tiles of queries. kPath: kAnyPage,
+// addresses are per lane; kPages16, a page holds a multiple of 16 tokens, so
+// half a block lies in one page, its address is the same for the whole wave,
+// and a lane's place in it is a 32-bit offset; kWhole, that and all kDim
+// dimensions are there. (8 heads of 80 dimensions, 671 MB: PATH_US.)
+enum { kAnyPage, kPages16, kWhole };
+
 // A step takes as many blocks as make 16 KB of keys and values (8 KB for 64
 // dimensions in 8 bits), the same registers whatever the type: the chain of a
 // step (products, maximum over the lanes, exponentials, products) is as long
@@ -189,8 +192,9 @@ __device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
 template <int kDim, int kElem, int kTiles>
 constexpr int kSubBlocks = kDim * kElem >= 256 || kTiles > 1 ? 1 : 2;
 
-template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast, bool kStream>
+template <typename T, bool kE4m3, int kDim, int kTiles, int kPath, bool kStream>
 struct Attender {
+    static constexpr bool kFast = kPath >= kPages16;
     static constexpr int kElem = kE4m3 ? 1 : 2;
     static constexpr int kStepsK = kDim / 32;                  // matrix steps per score
     static constexpr int kLoadsK = kE4m3 ? kDim / 64 : kDim / 32;
@@ -217,7 +221,7 @@ struct Attender {
     const uint8_t *kh, *vh;
     __amdgpu_buffer_rsrc_t score_rsrc;                         // this tile's rows of scores
     uint32_t score_lane[kTiles];
-    uint32_t k_lane, v_lane, token_bytes;                      // kFast: this lane's byte offsets
+    uint32_t k_lane, v_lane, token_bytes;                      // kFast: this lane's byte offsets in half a block
 
     uintx4 q[kTiles][kStepsK];
     int pos[kTiles];
@@ -292,26 +296,22 @@ struct Attender {
             return *reinterpret_cast<const W *>(p);
     }
 
+    // Dimension d of a token if there is one, else the first. What is read in
+    // its place is taken out of the keys where they are used, so that no load
+    // is waited for early, and gives values that are never written.
+    __device__ __forceinline__ uint32_t within(uint32_t d) const { return kPath == kWhole || d < a.c.dim ? d : 0; }
+
     __device__ __forceinline__ void load_k(const Place &p, uintx4 (&kr)[2][kLoadsK])
     {
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-            if constexpr (kFast) {
-                const uint8_t *base = kh + p.base[i] * kElem;
+            const uint8_t *base = kFast ? kh + p.base[i] * kElem + k_lane : kh + at_of(p, 16 * i + m) * kElem;
 #pragma unroll
-                for (int s = 0; s < kLoadsK; s++) kr[i][s] = fetch<uintx4>(base + k_lane + s * 64);
-            } else {
-                const uint8_t *base = kh + at_of(p, 16 * i + m) * kElem;
-#pragma unroll
-                for (int s = 0; s < kLoadsK; s++) {
-                    const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
-                    kr[i][s] = fetch<uintx4>(base + (d < a.c.dim ? d : 0) * kElem);
-                }
-#pragma unroll
-                for (int s = 0; s < kLoadsK; s++) {
-                    const uint32_t d = kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8;
-                    if (d >= a.c.dim) kr[i][s] = uintx4{0, 0, 0, 0};
-                }
+            for (int s = 0; s < kLoadsK; s++) {
+                if constexpr (kPath == kWhole)
+                    kr[i][s] = fetch<uintx4>(base + s * 64);
+                else
+                    kr[i][s] = fetch<uintx4>(base + within(kE4m3 ? s * 64 + g * 16 : s * 32 + g * 8) * kElem);
             }
         }
     }
@@ -328,8 +328,7 @@ struct Attender {
                 base = vh + at_of(p, (j >> 2) * 16 + g * 4 + (j & 3)) * kElem;
 #pragma unroll
             for (int h = 0; h < kParts; h++) {
-                const uint32_t d = h * 128 + m * kVd;
-                const uint8_t *src = kFast ? base + h * 128 * kElem : base + (d < a.c.dim ? d : 0) * kElem;
+                const uint8_t *src = kPath == kWhole ? base + h * 128 * kElem : base + within(h * 128 + m * kVd) * kElem;
                 if constexpr (kVw == 4) {
                     const uintx4 x = fetch<uintx4>(src);
 #pragma unroll
@@ -343,14 +342,6 @@ struct Attender {
                 }
             }
         }
-        if constexpr (!kFast)
-#pragma unroll
-            for (int h = 0; h < kParts; h++)
-                if (h * 128 + m * kVd >= (int)a.c.dim)
-#pragma unroll
-                    for (int j = 0; j < 8; j++)
-#pragma unroll
-                        for (int w = 0; w < kVw; w++) vr[j][h][w] = 0;
     }
 
     // All blocks of the wave. Keys of the next block are loaded as soon as
@@ -398,6 +389,8 @@ struct Attender {
                         } else {
                             kf = kr[i >> 1][i & 1][st];
                         }
+                        if constexpr (kPath != kWhole)
+                            if ((kE4m3 ? (st >> 1) * 64 + g * 16 : st * 32 + g * 8) >= (int)a.c.dim) kf = uintx4{0, 0, 0, 0};
                         s[t][i] = T::mfma(kf, q[t][st], s[t][i]);
                     }
                 }
@@ -569,11 +562,11 @@ struct Attender {
 template <int kWidth, int kSub, bool kFast>
 constexpr int kWaves = kWidth <= 64 ? (kSub == 1 || kFast ? 3 : 2) : kWidth <= 128 ? (kSub == 1 && kFast ? 3 : 2) : kWidth <= 256 && kFast ? 2 : 1;
 
-template <typename T, bool kE4m3, int kDim, int kTiles, bool kFast, bool kStream>
-__global__ __launch_bounds__(256, (kWaves<kDim == 256 ? 512 : kDim * kTiles, kSubBlocks<kDim, kE4m3 ? 1 : 2, kTiles>, kFast>))
+template <typename T, bool kE4m3, int kDim, int kTiles, int kPath, bool kStream>
+__global__ __launch_bounds__(256, (kWaves<kDim == 256 ? 512 : kDim * kTiles, kSubBlocks<kDim, kE4m3 ? 1 : 2, kTiles>, kPath == kWhole>))
 void attend_kernel(const DecodeArgs a)
 {
-    typedef Attender<T, kE4m3, kDim, kTiles, kFast, kStream> A;
+    typedef Attender<T, kE4m3, kDim, kTiles, kPath, kStream> A;
     constexpr int kRows = 16 * kTiles;
     constexpr int kPitch = kDim + 4;
 
@@ -633,8 +626,8 @@ void attend_kernel(const DecodeArgs a)
     w.kh = c.k + head * c.head_stride * A::kElem;
     w.vh = c.v + head * c.head_stride * A::kElem;
     w.token_bytes = (uint32_t)c.token_stride * A::kElem;
-    w.k_lane = m * w.token_bytes + g * 16;
-    w.v_lane = g * 4 * w.token_bytes + m * A::kVd * A::kElem;
+    w.k_lane = m * w.token_bytes + (kPath == kWhole ? g * 16 : 0);
+    w.v_lane = g * 4 * w.token_bytes + (kPath == kWhole ? m * A::kVd * A::kElem : 0);
     {
         const uint32_t rows = query_rows - tile * kRows < (uint32_t)kRows ? query_rows - tile * kRows : kRows;
         const uint64_t first = (((uint64_t)row * c.n_kv + head) * query_rows + tile * kRows) * a.score_len;
@@ -726,10 +719,13 @@ hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
 {
     const uint64_t grid = attend_grid(a);
     // lane offsets in half a block take 32 bits
-    if (a.c.page_size % 16 == 0 && a.c.dim == kDim && a.c.token_stride < (1u << 26))
-        attend_kernel<T, kE4m3, kDim, kTiles, true, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
+    const bool pages16 = a.c.page_size % 16 == 0 && a.c.token_stride < (1u << 26);
+    if (pages16 && a.c.dim == kDim)
+        attend_kernel<T, kE4m3, kDim, kTiles, kWhole, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
+    else if (pages16)
+        attend_kernel<T, kE4m3, kDim, kTiles, kPages16, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
     else
-        attend_kernel<T, kE4m3, kDim, kTiles, false, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
+        attend_kernel<T, kE4m3, kDim, kTiles, kAnyPage, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
