@@ -183,8 +183,8 @@ __device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
 // half a block lies in one page, its address is the same for the whole wave,
 // and a lane's place in it is a 32-bit offset; kWhole, that and all kDim
 // dimensions are there. (32 rows of 2,000 to 10,000 tokens, 8 heads in 16
-// bits: 128 dimensions 133 us, in pages of 24 tokens 148; 80 dimensions 167
-// us, in pages of 24 tokens 174.)
+// bits: 128 dimensions 133 us, in pages of 24 tokens 148; 80 dimensions 116
+// us, in pages of 24 tokens 128.)
 enum { kAnyPage, kPages16, kWhole };
 
 // A step takes as many blocks as make 16 KB of keys and values (8 KB for 64
@@ -288,7 +288,9 @@ struct Attender {
     // caches (16 heads of 128 dimensions in 16 bits: 380 -> 370 us for 2.1 GB,
     // 8 heads of 256: 348 -> 336 us, 20 query rows 216 -> 199 us; in 8 bits
     // 217 -> 222 us, 40 query rows, whose two units read the same, 268 -> 365
-    // us).
+    // us). Not where dimensions are missing: heads share lines, and the first
+    // dimensions are read again in place of the last (8 heads of 80: 116 us,
+    // streamed 160; of 192: 228 and 276).
     template <typename W>
     static __device__ __forceinline__ W fetch(const uint8_t *p)
     {
@@ -583,7 +585,9 @@ void attend_kernel(const DecodeArgs a)
     // pairs are under way at one time:
     //  - all heads of a slot on one die where a token's key is at most 128
     //    bytes, a cache line (8-bit, 8 heads: 64 dimensions 92 -> 69 us for
-    //    268 MB, 128 dimensions 119 -> 116 us for 537 MB);
+    //    268 MB, 128 dimensions 119 -> 116 us for 537 MB), or ends inside a
+    //    line (8 heads of 80 dimensions in 16 bits 128 -> 116 us for 481 MB,
+    //    of 96 130 -> 118 us for 577 MB);
     //  - all slots of few heads, up to 8 heads (8 heads of 128 dimensions in
     //    16 bits: 192 -> 177 us for 1.07 GB, three long rows 241 -> 222 us
     //    for 1.33 GB); the odd number of slots spreads a slot's heads over
@@ -722,12 +726,15 @@ hipError_t attend_page(const DecodeArgs &a, hipStream_t s)
     const uint64_t grid = attend_grid(a);
     // lane offsets in half a block take 32 bits
     const bool pages16 = a.c.page_size % 16 == 0 && a.c.token_stride < (1u << 26);
-    if (pages16 && a.c.dim == kDim)
+    const bool whole = a.c.dim == kDim;
+    if (pages16 && whole)
         attend_kernel<T, kE4m3, kDim, kTiles, kWhole, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
     else if (pages16)
-        attend_kernel<T, kE4m3, kDim, kTiles, kPages16, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
-    else
+        attend_kernel<T, kE4m3, kDim, kTiles, kPages16, false><<<(uint32_t)grid, 256, 0, s>>>(a);
+    else if (kStream && whole)
         attend_kernel<T, kE4m3, kDim, kTiles, kAnyPage, kStream><<<(uint32_t)grid, 256, 0, s>>>(a);
+    else
+        attend_kernel<T, kE4m3, kDim, kTiles, kAnyPage, false><<<(uint32_t)grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

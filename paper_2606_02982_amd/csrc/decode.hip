@@ -44,7 +44,7 @@ void decode_plan(DecodeArgs &a)
         a.n_slots = (uint32_t)(a.slot_goal + a.n_rows < most ? a.slot_goal + a.n_rows : most);
     }
     // a die per slot needs slots for every die
-    a.spread = key_bytes <= 128 && a.n_slots >= 64 ? kDieOfSlot : a.c.n_kv <= 8 ? kSlotsFirst : kHeadsFirst;
+    a.spread = (key_bytes <= 128 || key_bytes % 128) && a.n_slots >= 64 ? kDieOfSlot : a.c.n_kv <= 8 ? kSlotsFirst : kHeadsFirst;
 }
 
 static uint64_t part_rows_of(const DecodeArgs &a) { return (uint64_t)a.n_slots * a.c.n_kv * a.n_tiles * a.part_rows; }
