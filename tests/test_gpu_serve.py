@@ -302,6 +302,31 @@ def test_attention_nonfinite_seen(ds):
     assert torch.isinf(out[0, 0, :, :7]).all() and torch.isnan(out[1]).all() and (out[2] == 0).all()
 
 
+@pytest.mark.parametrize("kt", [BF16, E4M3])
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("dim", [48, 80, 96, 144, 240])
+def test_attention_nonfinite_first_dims(ds, dim, page, kt):
+    """Infinities (NaN in 8 bits) in a token's first dimensions stay there,
+    also where dimensions do not fill a tile: a score of -inf is no weight, a
+    value's infinity reaches its own dimension alone."""
+    bad = float("nan") if kt == E4M3 else float("inf")
+    s = Setup(ds, [70, 700, 70], page, 2, dim, kt, seed=10)
+    spot = lambda r, j: (int(s.table[r, j // page]), j % page)
+    for r in (0, 1):
+        pg, sl = spot(r, 30)
+        s.v[pg, sl, 1, 0] = bad
+    if kt == BF16:
+        pg, sl = spot(2, 7)
+        s.k[pg, sl, :, 0] = -float("inf")
+    s.push()
+    q = queries(s, 3, 2, 4, dim, BF16)
+    q[..., 0] = 1.0
+    out = s.attend(ds, q)
+    assert not torch.isfinite(out[:2, :, 2:, 0]).any() and torch.isfinite(out[:2, :, :, 1:]).all()
+    assert torch.isfinite(out[2]).all()
+    s.attend(ds, q, mass=torch.zeros((3, 2, 700)), max_len=700)
+
+
 def test_attention_far_offsets(ds):
     """Pages more than 2^32 elements apart."""
     page, n_kv, dim = 16, 1, 64
