@@ -562,12 +562,15 @@ struct Attender {
     uint32_t req;
 };
 
-// Waves per SIMD that the registers are limited to: as many as fit without spills.
+// Waves per SIMD that the registers are limited to: as many as fit without
+// spills. kFast: kWhole, and kPages16 with two tiles of query rows (24 rows, 8
+// heads of 80 dimensions, 671 MB: 161 us, with one wave less 171; for one tile
+// 125 us for 481 MB, with one wave less 116).
 template <int kWidth, int kSub, bool kFast>
 constexpr int kWaves = kWidth <= 64 ? (kSub == 1 || kFast ? 3 : 2) : kWidth <= 128 ? (kSub == 1 && kFast ? 3 : 2) : kWidth <= 256 && kFast ? 2 : 1;
 
 template <typename T, bool kE4m3, int kDim, int kTiles, int kPath, bool kStream>
-__global__ __launch_bounds__(256, (kWaves<kDim == 256 ? 512 : kDim * kTiles, kSubBlocks<kDim, kE4m3 ? 1 : 2, kTiles>, kPath == kWhole>))
+__global__ __launch_bounds__(256, (kWaves<kDim == 256 ? 512 : kDim * kTiles, kSubBlocks<kDim, kE4m3 ? 1 : 2, kTiles>, kPath == kWhole || (kPath == kPages16 && kTiles > 1)>))
 void attend_kernel(const DecodeArgs a)
 {
     typedef Attender<T, kE4m3, kDim, kTiles, kPath, kStream> A;
