@@ -111,6 +111,10 @@ __device__ inline void pick_digit(Select &sm, uint32_t want)
 // on one compute unit (24 selections of 60,000 to 100,000 tokens 90 us; 256
 // of 2,048 to 6,144 17 us) and, for few tokens, into a chain of barriers
 // (700 tokens 9 us; with all counts of a bin in one bank 21 us).
+// A request that stands in two rows, against the contract, is compacted in
+// place by one workgroup while another still selects, so that what one pass
+// counted the next may not find again: places in the list, in kept and among
+// the masses are therefore held in their bounds one by one.
 __device__ inline void select_tokens(const EvictArgs &a, const Cut &x, const float *mass, float *mass_out, uint32_t *kept, Select &sm)
 {
     const uint32_t n = x.n, lo = a.sinks, span = n - a.recent - a.sinks;   // the tokens that compete
@@ -165,10 +169,11 @@ __device__ inline void select_tokens(const EvictArgs &a, const Cut &x, const flo
                 uint32_t to = 0;
                 if (lane == 0) to = atomicAdd(&sm.listed, (uint32_t)__popcll(all));
                 to = readlane32(to, 0) + (uint32_t)__popcll(all & lanemask_lt());
-                if (on) sm.list[to] = key;
+                if (on && to < kList) sm.list[to] = key;
             });
             __syncthreads();
         }
+        const uint32_t listed = sm.listed < kList ? sm.listed : kList;
 #pragma unroll 1
         for (int shift = 10; shift >= 0; shift -= 10) {
             // bits 20 .. 10, then 9 .. 0
@@ -179,7 +184,7 @@ __device__ inline void select_tokens(const EvictArgs &a, const Cut &x, const flo
                 if (key >> above == found) count((key >> shift) & mask);
             };
             if (fits)
-                for (uint32_t i = threadIdx.x; i < sm.listed; i += kSelect) look(sm.list[i]);
+                for (uint32_t i = threadIdx.x; i < listed; i += kSelect) look(sm.list[i]);
             else
                 groups([&](uint32_t j, float v) {
                     if (j - lo < span) look(mass_key(v));
@@ -227,7 +232,7 @@ __device__ inline void select_tokens(const EvictArgs &a, const Cut &x, const flo
         }
         const uint64_t all = __ballot(stays);
         const uint32_t to = at + (uint32_t)__popcll(all & lanemask_lt());
-        if (stays) {
+        if (stays && to < x.keep) {
             kept[to] = j;
             if (direct) mass_out[to] = v;
         }
@@ -242,7 +247,8 @@ __device__ inline void select_tokens(const EvictArgs &a, const Cut &x, const flo
 #pragma unroll
         for (int k = 0; k < kPiece; k++) {
             const uint32_t p = i + k * kSelect + threadIdx.x;
-            v[k] = p < x.keep ? mass[kept[p]] : 0.0f;
+            const uint32_t from = p < x.keep ? kept[p] : 0;
+            v[k] = from < n ? mass[from] : 0.0f;
         }
         __syncthreads();
 #pragma unroll
@@ -579,6 +585,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const EvictArgs a, uint32_t g
         }
         for (uint32_t i = threadIdx.x; i < count * units; i += 256) {
             const uint32_t to = first + i / units, from = kept[to], u = i % units;
+            if (from >= x.n) continue;     // an entry that no selection wrote (select_tokens)
             const uint32_t sp = s.table[(uint64_t)x.req * s.max_pages + from / s.page_size];
             const uint32_t dp = d.table[(uint64_t)row * d.max_pages + to / d.page_size];
             if (sp >= s.n_pages || dp >= d.n_pages) continue;

@@ -1,0 +1,52 @@
+"""The decode step where device data break a stated contract: unspecified
+results, but nothing is written or read outside what the call names."""
+import pytest
+import torch
+
+from tests.test_gpu_serve import BF16, Setup
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ds():
+    from paper_2606_02982_amd import driftsched
+    return driftsched
+
+
+@pytest.mark.parametrize("kind", ["spread", "one digit", "equal", "zeros"])
+@pytest.mark.parametrize("n,share,inplace", [(20000, 0.5, True), (20000, 0.95, True), (3000, 0.3, True), (300, 0.6, True),
+                                             (20000, 0.5, False), (30000, 0.5, True)])
+def test_evict_request_in_many_rows(ds, kind, n, share, inplace):
+    """Rows of one request are selected for at the same time, in place: one
+    compacts the masses that another still counts."""
+    per, n_rows, n_kv = -(-n // 64), 24, 2
+    s = Setup(ds, [n, 100, n], 64, n_kv, 16, BF16, seed=n)
+    r = torch.rand((3, n_kv, per * 64), generator=s.g)
+    mass = {"spread": (4 * r).exp(), "one digit": 1.0 + r * 2.0 ** -3, "equal": torch.full_like(r, 0.5),
+            "zeros": torch.where(r < 0.5, 0.0, r)}[kind].contiguous()
+    rows = torch.tensor([0, 2] * (n_rows // 2), dtype=torch.int32)
+    keep = int(n * share)
+    budget = torch.tensor([keep, 100, keep], dtype=torch.float64)
+    pool = [torch.zeros((n_rows * per + 1,) + tuple(s.k.shape[1:]), dtype=BF16, device="cuda") for _ in range(2)]
+    table = torch.arange(n_rows * per, dtype=torch.int32).view(n_rows, per)
+    dst = ds.kv_cache(*pool, table.cuda(), torch.zeros(n_rows, dtype=torch.int32, device="cuda"))
+    for left_over in (-1, 0x7FFFFFFF, 12345678):          # what kept holds before the call
+        on = mass.cuda()
+        out = on if inplace else torch.full_like(on, 5.0)
+        kept = torch.full((n_rows, n_kv, per * 64 + 8), left_over, dtype=torch.int32, device="cuda")
+        left, kept = ds.cache_evict(s.cache, dst, budget.cuda(), on, rows=rows.cuda(), sinks=4, recent=16,
+                                    mass_out=None if inplace else out, kept=kept)
+        assert (left == keep).all()
+        assert (kept[:, :, keep:] == left_over).all()
+        written = kept[:, :, :keep]
+        assert ((written >= 0) & (written < n) | (written == left_over)).all()
+        rest = mass if inplace else torch.full_like(mass, 5.0)
+        assert torch.equal(out[:, :, keep:].cpu(), rest[:, :, keep:]) and torch.equal(out[1].cpu(), rest[1])
+        for x in pool:
+            assert (x[-1] == 0).all()
+            assert (x[:-1].view(n_rows, per * 64, n_kv, 16)[:, keep:] == 0).all()
+    with pytest.raises(ds.DriftSchedError):
+        ds.cache_evict(s.cache, dst, budget.cuda(), mass.cuda(), rows=rows.cuda(), validate=True)
+    # the same rows one by one are right
+    ds.cache_evict(s.cache, dst, budget.cuda(), mass.cuda(), rows=rows[:2].cuda().contiguous(), sinks=4, recent=16, validate=True)
