@@ -153,6 +153,8 @@ typedef struct {
  * cut must be distinct and not among those that hold the batch's tokens. k and
  * v of dst may be those of src (one pool), and the caller then enters dst's
  * pages in the request's own table.
+ *  dst->len may not overlap src->len (DS_ERR_ARG): the caller takes the new
+ *  lengths over together with the pages.
  *
  *  src, dst   same page_size, n_kv, head_dim, type and strides; dst has one
  *             request per row (dst->n_requests >= n_rows) and len is written

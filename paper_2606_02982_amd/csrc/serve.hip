@@ -59,6 +59,12 @@ ds_status pointers_of(const KvView &v)
     return DS_OK;
 }
 
+bool overlap(const void *a, uint64_t a_bytes, const void *b, uint64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
 ds_status decode_args(const ds_kv_cache *cache, const ds_decode_params *p, uint32_t n_rows, DecodeArgs &a)
 {
     if (!p) return DS_ERR_NULL;
@@ -202,6 +208,8 @@ ds_status ds_cache_evict(const ds_kv_cache *src, const ds_kv_cache *dst, const d
         return DS_ERR_ALIGN;
     st = check_scratch(ws, ws_bytes, evict_ws_bytes(a), flags);
     if (st != DS_OK) return st;
+    // every launch looks up again which rows are cut: their lengths may not change on the way
+    if (overlap(a.src.len, (uint64_t)a.src.n_requests * 4, a.dst.len, (uint64_t)n_rows * 4)) return DS_ERR_ARG;
     a.rows = rows;
     a.budget = budget;
     a.mass = mass;

@@ -716,7 +716,7 @@ def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0
     ``dst``: a ``kv_cache`` of the same layout whose row i names the fresh
     pages of row i (its k and v may be the pool of ``cache``); ``dst.lens[i]``
     receives the row's new length, which is smaller than before exactly where
-    the row was cut and copied. ``budget``: float64 (n_requests), e.g. from
+    the row was cut and copied; dst.lens may not be (part of) cache.lens. ``budget``: float64 (n_requests), e.g. from
     ``score``. ``mass``: as ``decode_attention`` leaves it. ``mass_out``: None
     updates mass in place. ``kept``: int32 (n_rows, n_kv, length); by default
     as long as dst's rows. Returns (dst.lens, kept)."""

@@ -50,3 +50,29 @@ def test_evict_request_in_many_rows(ds, kind, n, share, inplace):
         ds.cache_evict(s.cache, dst, budget.cuda(), mass.cuda(), rows=rows.cuda(), validate=True)
     # the same rows one by one are right
     ds.cache_evict(s.cache, dst, budget.cuda(), mass.cuda(), rows=rows[:2].cuda().contiguous(), sinks=4, recent=16, validate=True)
+
+
+@pytest.mark.parametrize("n", [300, 30000])
+def test_evict_lengths_side_by_side(ds, n):
+    """The new lengths next to the old ones in one tensor; the old ones
+    themselves are refused, and nothing has changed then."""
+    s = Setup(ds, [n, 40, n - 7], 64, 2, 16, BF16, seed=n)
+    per = s.table.shape[1]
+    mass = torch.rand((3, 2, per * 64), generator=s.g)
+    budget = torch.tensor([n * 0.5, 100.0, n * 0.75], dtype=torch.float64).cuda()
+    lens = torch.cat([s.lens, torch.zeros(5, dtype=torch.int32)]).cuda()
+    pool = [torch.zeros((3 * per,) + tuple(s.k.shape[1:]), dtype=BF16, device="cuda") for _ in range(2)]
+    pages = torch.arange(3 * per, dtype=torch.int32).view(3, per).cuda()
+    src = ds.kv_cache(s.dk, s.dv, s.cache.table, lens[:3])
+    on = mass.cuda()
+    for shared, rows in ((lens[:3], None), (lens[2:5], None), (lens[1:4], torch.arange(3, dtype=torch.int32).cuda())):
+        with pytest.raises(ds.DriftSchedError) as e:
+            ds.cache_evict(src, ds.kv_cache(*pool, pages, shared), budget, on, rows=rows)
+        assert e.value.status == -2
+    assert lens.tolist() == s.lens.tolist() + [0] * 5 and torch.equal(on.cpu(), mass) and not pool[0].any()
+    left, kept = ds.cache_evict(src, ds.kv_cache(*pool, pages, lens[3:6]), budget, on, validate=True)
+    want = [n // 2, 40, int((n * 0.75))]
+    assert left.tolist() == want and lens.tolist() == s.lens.tolist() + want + [0, 0]
+    assert torch.equal(on[0, :, :want[0]].cpu(), mass[0].gather(1, kept[0, :, :want[0]].cpu().long()))
+    assert torch.equal(pool[0][pages[0].long()].flatten(0, 1)[torch.arange(want[0]), 1].cpu(),
+                       s.k[s.table[0].long()].flatten(0, 1)[kept[0, 1, :want[0]].cpu().long(), 1])
