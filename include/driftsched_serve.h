@@ -111,8 +111,9 @@ typedef struct {
  * Nothing is written from entry n on.
  *
  * Scores, softmax and sums are held in 32 bits; the weights enter the second
- * product as two 16-bit parts, so that out is rounded once, at the end. The
- * same inputs give the same bits on every run.
+ * product as two parts of q's type, which hold a weight to 2^-17 (bfloat16) or
+ * 2^-22 (float16, and to 2^-40 of the query's largest weight), so that out is
+ * rounded once, at the end. The same inputs give the same bits on every run.
  *
  *  q    device, q_type, element (i, t, h, d) at i * q_row_stride + t *
  *       q_token_stride + h * q_head_stride + d; 16-byte aligned

@@ -22,7 +22,9 @@
 //    registers to get one dimension of eight tokens.
 // Weights are split into two 16-bit parts (value and remainder), so that
 // rounding them adds nothing to out's own rounding; the matrix units are idle
-// most of the time anyway.
+// most of the time anyway. float16 has no step below 2^-24, so there the
+// weights are taken times 2^15 (at most 32,768): what both parts lose is below
+// 2^-40 of the largest weight instead of 2^-25.
 #pragma once
 
 #include "common.h"
@@ -36,6 +38,7 @@ typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
 
 struct Bf16 {
+    static constexpr float kWeight = 1.0f;         // what weights are multiplied with before they are split
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ floatx4 mfma(uintx4 a, uintx4 b, floatx4 c)
@@ -58,6 +61,7 @@ struct Bf16 {
 };
 
 struct F16 {
+    static constexpr float kWeight = 32768.0f;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ floatx4 mfma(uintx4 a, uintx4 b, floatx4 c)
@@ -482,6 +486,7 @@ struct Attender {
                     for (int e = 0; e < 4; e++) {
                         s[t][i][e] = __builtin_amdgcn_exp2f(s[t][i][e] - base);
                         sum[t] += s[t][i][e];
+                        if constexpr (T::kWeight != 1.0f) s[t][i][e] *= T::kWeight;
                     }
 #pragma unroll
                 for (int i = 0; i < 2 * kSub; i++)
@@ -674,6 +679,7 @@ void attend_kernel(const DecodeArgs a)
     auto &sum = w.sum;
     auto &acc = w.acc;
     constexpr int kVd = A::kVd;
+    constexpr float kOff = 1.0f / T::kWeight;
     // the waves' results side by side; they are joined as they are read
 #pragma unroll
     for (int t = 0; t < kTiles; t++) {
@@ -690,7 +696,7 @@ void attend_kernel(const DecodeArgs a)
 #pragma unroll
                 for (int x = h * kVd; x < (h + 1) * kVd; x += 4)
                     *reinterpret_cast<floatx4 *>(&sm_o[wave][(t * 16 + m) * kPitch + h * 128 + (g * 4 + e) * kVd + x % kVd]) =
-                        floatx4{acc[t][x][e], acc[t][x + 1][e], acc[t][x + 2][e], acc[t][x + 3][e]};
+                        floatx4{acc[t][x][e] * kOff, acc[t][x + 1][e] * kOff, acc[t][x + 2][e] * kOff, acc[t][x + 3][e] * kOff};
     }
     __syncthreads();
     const uint32_t rows_here = query_rows - tile * kRows < (uint32_t)kRows ? query_rows - tile * kRows : kRows;

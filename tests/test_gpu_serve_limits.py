@@ -1,0 +1,61 @@
+"""The decode step at the ends of its number ranges: weights far below the
+largest, values near the end of their type."""
+import math
+
+import pytest
+import torch
+
+from tests import serve_ref as ref
+from tests.test_gpu_serve import E4M3, F16, Setup
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ds():
+    from paper_2606_02982_amd import driftsched
+    return driftsched
+
+
+def relative(n, dim, size):
+    """Of a weight: its own score's and the normalizer's error (dim products
+    summed in 32 bits, the scale, the exponential's argument and value), and
+    sums over n tokens in 32 bits."""
+    return 2 * (dim + 8) * EPS * max(1.0, size) + (n + 64) * EPS
+
+
+@pytest.mark.parametrize("kt", [F16, E4M3])
+@pytest.mark.parametrize("n,gap,t,group,dim", [
+    (33, 18, 1, 1, 64), (700, 16, 1, 1, 64), (700, 20, 4, 6, 64), (4000, 20, 1, 4, 128), (4000, 24, 5, 8, 128), (4000, 24, 1, 1, 80),
+    (4000, 22, 1, 2, 256), (40000, 26, 1, 4, 64), (131072, 28, 1, 1, 64)])
+@pytest.mark.parametrize("window", [0, 500])
+def test_small_weights_of_f16(ds, n, gap, t, group, dim, kt, window):
+    """Every 32nd token takes nearly all the weight and has the value 0, the
+    others stand `gap` - 0.375 bits below: out is the others' part alone."""
+    s = Setup(ds, [n], 64, 1, dim, kt, seed=n + gap)
+    j = torch.arange(n)
+    at = s.table[0].long()[j // 64], j % 64
+    key = torch.zeros(n, dim)
+    key[:, 0] = torch.where(j % 32 == 0, gap, 0.375)
+    val = 256.0 * (0.5 + torch.rand((n, dim), generator=s.g))
+    val[::32] = 0.0
+    for pool, x in ((s.k, key), (s.v, val)):
+        whole = pool.float()
+        whole[at[0], at[1], 0] = x
+        pool.copy_(whole.to(kt))
+    scales = {}
+    if kt == E4M3:
+        scales = dict(k_scale=torch.ones(1), v_scale=torch.full((1,), 64.0))
+    s.push()
+    s.cache = ds.kv_cache(s.dk, s.dv, s.table.cuda(), s.lens.cuda(), *[x.cuda() for x in scales.values()])
+    q = torch.zeros((1, t, group, dim))
+    q[..., 0] = 1.0
+    q = q.to(F16)
+    out = ds.decode_attention(q.cuda(), s.cache, scale=math.log(2.0), window=window, max_len=n, validate=True)
+    want, _, _, _ = ref.attention(q, s.k, s.v, s.table, s.lens, scale=math.log(2.0), window=window, **scales)
+    # a weight's f16 parts hold it to 2^-22, or to 2^-40 of the largest
+    seen = min(n, window or n)
+    off = (relative(seen, dim, gap) + 2.0 ** -22) * abs(want) + seen * 2.0 ** -40 * 384 * (64 if scales else 1)
+    ref.check_out(out.cpu(), want, off, F16)
