@@ -4,8 +4,9 @@
 // With q scaled by scale * log2(e), every query keeps the running maximum m
 // of its scores s_j, the sum l = sum_j 2^(s_j - m) and o = sum_j 2^(s_j - m)
 // v_j, and rescales l and o when m grows; out = o / l. Splits of the cache
-// and the four waves of a workgroup hold (m, l, o) of their own tokens and
-// are joined by the same rule.
+// and the four waves of a workgroup hold (m, l, o / l) of their own tokens and
+// are joined by the same rule: o / l is a mean of values and so no larger than
+// the largest of them, while o of values near the type's end may pass it.
 //
 // The work is reading the cache once: 4 dim bytes per token and head in 16
 // bits against 4 dim flops per query row. So the loop is laid out for loads:
@@ -202,6 +203,7 @@ template <typename T, bool kE4m3, int kDim, int kTiles, int kPath, bool kStream>
 struct Attender {
     static constexpr bool kFast = kPath >= kPages16;
     static constexpr int kElem = kE4m3 ? 1 : 2;
+    static constexpr bool kWideValues = !kE4m3 && T::kWeight == 1.0f;   // bfloat16
     static constexpr int kStepsK = kDim / 32;                  // matrix steps per score
     static constexpr int kLoadsK = kE4m3 ? kDim / 64 : kDim / 32;
     static constexpr int kParts = kDim > 128 ? kDim / 128 : 1; // V: pieces of a row
@@ -223,6 +225,7 @@ struct Attender {
     uint32_t row, head, tile, query_rows, n;
     int m, g, first_pos, lo;
     float scale;
+    float down;                                                // what kCareful multiplies values with
     ScalarU32 table;
     const uint8_t *kh, *vh;
     __amdgpu_buffer_rsrc_t score_rsrc;                         // this tile's rows of scores
@@ -357,8 +360,8 @@ struct Attender {
     // product has: while one is waited for the other is under way.
     // kCareful: 0 * inf or 0 * NaN of a token that some queries do not see
     // must not reach their sums, so every product is made only where the
-    // weight is not 0 (taken where the first pass gave a number that is not
-    // finite).
+    // weight is not 0, and with values small enough for their sum (taken
+    // where the first pass gave a number that is not finite).
     template <bool kCareful>
     __device__ __forceinline__ void pass(uint32_t v, uint32_t v1)
     {
@@ -547,7 +550,7 @@ struct Attender {
 #pragma unroll
                                             for (int i = 0; i < 4; i++) {
                                                 const uint32_t w = (uint32_t)__shfl((int)vf[j >> 1], from * 16 + g * 4 + i, 64);
-                                                const float val = (j & 1) ? T::hi(w) : T::lo(w);
+                                                const float val = ((j & 1) ? T::hi(w) : T::lo(w)) * down;
                                                 if (pw != 0.0f) acc[t][x][i] += pw * val;
                                             }
                                         }
@@ -635,6 +638,9 @@ void attend_kernel(const DecodeArgs a)
     w.g = g;
     w.first_pos = first_pos;
     w.lo = a.window && first_pos >= (int)a.window ? first_pos - (int)a.window + 1 : 0;
+    // sums of float16 and of 8-bit values are far from the end of 32 bits
+    w.down = 1.0f;
+    if constexpr (A::kWideValues) w.down = __builtin_amdgcn_ldexpf(1.0f, __builtin_clz((v1 - v0) * kBlockTokens | 1) - 32);
     w.scale = a.scale2 * (kE4m3 && c.k_scale ? c.k_scale[head] : 1.0f);
     w.table = (ScalarU32)(uint64_t)(c.table + (uint64_t)req * c.max_pages);
     w.kh = c.k + head * c.head_stride * A::kElem;
@@ -679,12 +685,13 @@ void attend_kernel(const DecodeArgs a)
     auto &sum = w.sum;
     auto &acc = w.acc;
     constexpr int kVd = A::kVd;
-    constexpr float kOff = 1.0f / T::kWeight;
+    const float times = T::kWeight * (__any(odd) ? w.down : 1.0f);      // acc is o times this
     // the waves' results side by side; they are joined as they are read
 #pragma unroll
     for (int t = 0; t < kTiles; t++) {
         sum[t] += __shfl_xor(sum[t], 16, 64);
         sum[t] += __shfl_xor(sum[t], 32, 64);
+        const float inv = sum[t] == 0.0f ? 0.0f : 1.0f / (sum[t] * times);
         if (g == 0) {
             sm_m[wave][t * 16 + m] = mx[t];
             sm_l[wave][t * 16 + m] = sum[t];
@@ -696,7 +703,7 @@ void attend_kernel(const DecodeArgs a)
 #pragma unroll
                 for (int x = h * kVd; x < (h + 1) * kVd; x += 4)
                     *reinterpret_cast<floatx4 *>(&sm_o[wave][(t * 16 + m) * kPitch + h * 128 + (g * 4 + e) * kVd + x % kVd]) =
-                        floatx4{acc[t][x][e] * kOff, acc[t][x + 1][e] * kOff, acc[t][x + 2][e] * kOff, acc[t][x + 3][e] * kOff};
+                        floatx4{acc[t][x][e] * inv, acc[t][x + 1][e] * inv, acc[t][x + 2][e] * inv, acc[t][x + 3][e] * inv};
     }
     __syncthreads();
     const uint32_t rows_here = query_rows - tile * kRows < (uint32_t)kRows ? query_rows - tile * kRows : kRows;
@@ -705,26 +712,31 @@ void attend_kernel(const DecodeArgs a)
         float top = sm_m[0][rr], l = 0.0f;
 #pragma unroll
         for (int k = 1; k < 4; k++) top = fmaxf(top, sm_m[k][rr]);
+        float share[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            // a wave without tokens has a share of 0 and means of 0
+            share[k] = sm_l[k][rr] * __builtin_amdgcn_exp2f(sm_m[k][rr] - finite_or_zero(top));
+            l += share[k];
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         floatx4 o = {0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            // a wave without tokens has f = 0 and sums of zeros
-            const float f = __builtin_amdgcn_exp2f(sm_m[k][rr] - finite_or_zero(top));
-            l += sm_l[k][rr] * f;
             const floatx4 x = *reinterpret_cast<const floatx4 *>(&sm_o[k][rr * kPitch + d]);
 #pragma unroll
-            for (int e = 0; e < 4; e++) o[e] += x[e] * f;
+            for (int e = 0; e < 4; e++) o[e] += x[e] * (share[k] * inv);
         }
         const uint64_t at = ((uint64_t)pair * a.n_tiles + tile) * a.part_rows + rr;
         if (a.part_ml && d == 0) *reinterpret_cast<floatx2 *>(a.part_ml + 2 * at) = floatx2{top, l};
         if (slots.count > 1) {
             *reinterpret_cast<floatx4 *>(a.part_o + at * kDim + d) = o;
         } else if (d < c.dim) {
-            const float inv = l == 0.0f ? 0.0f : (kE4m3 && c.v_scale ? c.v_scale[head] : 1.0f) / l;
+            const float times = kE4m3 && c.v_scale ? c.v_scale[head] : 1.0f;
             const uint32_t r = tile * kRows + rr, tok = r / a.group, h = r % a.group;
             uint16_t *to = static_cast<uint16_t *>(a.out) +
                            (((uint64_t)row * a.tokens + tok) * c.n_kv * a.group + (uint64_t)head * a.group + h) * c.dim + d;
-            *reinterpret_cast<uintx2 *>(to) = uintx2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+            *reinterpret_cast<uintx2 *>(to) = uintx2{T::pack(o[0] * times, o[1] * times), T::pack(o[2] * times, o[3] * times)};
         }
     }
 }

@@ -108,11 +108,12 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t 
         const uint32_t team = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
         const float *from = a.part_o + at * kDim + d, *m = a.part_ml + 2 * at;
         const floatx2 ml = join_ml<kLanes>(m, stride, count);
-        const float base = finite_or_zero(ml[0]);
+        const float base = finite_or_zero(ml[0]), inv = ml[1] == 0.0f ? 0.0f : 1.0f / ml[1];
         floatx4 o = {0, 0, 0, 0};
 #pragma unroll 8
         for (uint32_t s = team; s < count; s += kTeams) {
-            const float f = __builtin_amdgcn_exp2f(m[2 * s * stride] - base);
+            const floatx2 y = *reinterpret_cast<const floatx2 *>(m + 2 * s * stride);
+            const float f = __builtin_amdgcn_exp2f(y[0] - base) * y[1] * inv;
             const floatx4 x = *reinterpret_cast<const floatx4 *>(from + s * stride * kDim);
 #pragma unroll
             for (int e = 0; e < 4; e++) o[e] += f * x[e];
@@ -125,11 +126,11 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs a, uint32_t 
 #pragma unroll
                 for (int e = 0; e < 4; e++) o[e] += x[e];
             }
-            const float inv = ml[1] == 0.0f ? 0.0f : (c.type == DS_E4M3 && c.v_scale ? c.v_scale[head] : 1.0f) / ml[1];
+            const float times = c.type == DS_E4M3 && c.v_scale ? c.v_scale[head] : 1.0f;
             const uint32_t tok = r / a.group, h = r % a.group;
             uint16_t *to = static_cast<uint16_t *>(a.out) +
                            (((uint64_t)row * a.tokens + tok) * c.n_kv * a.group + (uint64_t)head * a.group + h) * c.dim + d;
-            *reinterpret_cast<uintx2 *>(to) = uintx2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+            *reinterpret_cast<uintx2 *>(to) = uintx2{T::pack(o[0] * times, o[1] * times), T::pack(o[2] * times, o[3] * times)};
         }
         return;
     }

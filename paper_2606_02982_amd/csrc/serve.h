@@ -41,7 +41,7 @@ struct DecodeArgs {
     int spread;            // order of the pairs (attend_kernel)
     uint32_t part_rows;    // query rows of a unit's partial result
     uint32_t score_len;    // tokens of a row of scores
-    float *part_o;         // (unit, part_rows, padded dim); a row in one slot has none
+    float *part_o;         // (unit, part_rows, padded dim): mean values; a row in one slot has none
     float *part_ml;        // (unit, part_rows, 2): running maximum and sum
     uint32_t *row_slots;   // (row, 2): its first slot and their number
     float *scores;         // (row, head, query row, score_len), for mass

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests import serve_ref as ref
-from tests.test_gpu_serve import E4M3, F16, Setup
+from tests.test_gpu_serve import BF16, E4M3, F16, Setup
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +59,27 @@ def test_small_weights_of_f16(ds, n, gap, t, group, dim, kt, window):
     seen = min(n, window or n)
     off = (relative(seen, dim, gap) + 2.0 ** -22) * abs(want) + seen * 2.0 ** -40 * 384 * (64 if scales else 1)
     ref.check_out(out.cpu(), want, off, F16)
+
+
+@pytest.mark.parametrize("n", [2, 100, 3000, 20000])
+@pytest.mark.parametrize("t,group,dim", [(1, 1, 128), (3, 4, 64), (5, 8, 128), (1, 2, 80), (2, 2, 256)])
+@pytest.mark.parametrize("page", [16, 24])
+def test_values_near_the_end_of_bf16(ds, n, t, group, dim, page):
+    """A mean of values is no larger than the largest of them, however many
+    they are; dimensions of ordinary and of small values keep theirs."""
+    s = Setup(ds, [n, 50, n], page, 1, dim, BF16, seed=n)
+    size = torch.ones(dim)
+    size[0::4], size[1::4], size[2::4] = 3.0e38, -1.0e38, 2.0 ** -100
+    s.v.copy_((s.v.float().abs().clamp(0.5, 1.0) * size).to(BF16))
+    # of the last request one token has an infinite value in the last dimension
+    p = int(s.table[2, 0])
+    s.v[p, 0, 0, dim - 1] = float("inf")
+    s.push()
+    q = (0.5 * torch.randn((3, t, group, dim), generator=s.g)).to(BF16)
+    mass = torch.zeros((3, 1, max(n, 50)))
+    dm = mass.cuda()
+    out = ds.decode_attention(q.cuda(), s.cache, mass=dm, max_len=max(n, 50), validate=True)
+    want, off, m, m_off = ref.attention(q, s.k, s.v, s.table, s.lens, mass=mass)
+    assert torch.isfinite(out[:2]).all() and torch.isfinite(out[2, ..., :dim - 1]).all()
+    ref.check_out(out.cpu(), want, off, BF16)
+    ref.check_mass(dm.cpu(), m, m_off)
