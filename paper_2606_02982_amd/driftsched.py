@@ -605,6 +605,13 @@ def _arg(t, index, dtype, shape, name):
     return t.data_ptr()
 
 
+def _refuse_counts(**counts):
+    """Names the first that a count of the C structs (32 bits, unsigned) does not hold."""
+    for name, x in counts.items():
+        if not 0 <= x <= 0xFFFFFFFF or int(x) != x:
+            raise ValueError("%s must be a whole number from 0 to 2^32 - 1, got %r" % (name, x))
+
+
 def _scratch(ws, need, like, index, validate):
     """Address and size of the workspace, and what holds it: the caller's, or
     one of this call alone, taken from torch's allocator on the current stream,
@@ -685,6 +692,8 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
     float32 (n_requests, n_kv, length >= max_len), updated in place with the
     weight each cached token received. ``out`` must not overlap q. Returns out,
     shaped like q."""
+    if type(window) is not int or type(sinks) is not int or type(max_len) is not int or (window | sinks | max_len) >> 32:
+        _refuse_counts(window=window, sinks=sinks, max_len=max_len)
     if q.dim() != 4 or q.shape[3] != cache.head_dim or q.stride(3) != 1:
         raise ValueError("q must be (n_rows, n_tokens, n_q, head_dim) with a dense last axis")
     if q.dtype is not torch.bfloat16 and q.dtype is not torch.float16:
@@ -720,6 +729,8 @@ def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0
     ``score``. ``mass``: as ``decode_attention`` leaves it. ``mass_out``: None
     updates mass in place. ``kept``: int32 (n_rows, n_kv, length); by default
     as long as dst's rows. Returns (dst.lens, kept)."""
+    if any(type(x) is not int or x >> 32 for x in (sinks, recent, slack, max_len)):
+        _refuse_counts(sinks=sinks, recent=recent, slack=slack, max_len=max_len)
     dev = _device_of(budget)
     if dev != cache.index or dev != dst.index:
         raise ValueError("budget and the caches must be on one device")
