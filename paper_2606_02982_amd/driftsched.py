@@ -648,8 +648,8 @@ def kv_cache(k, v, table, lens, k_scale=None, v_scale=None):
     """A paged key-value cache for ``decode_attention`` and ``cache_evict``.
 
     ``k``, ``v``: (n_pages, page_size, n_kv, head_dim), float16, bfloat16 or
-    float8_e4m3fn, with the same strides; any order of the first three axes in
-    memory, the last one dense. ``table``: int32 (n_requests, max_pages), the
+    float8_e4m3fn, with the same strides, multiples of 16 bytes; any order of
+    the first three axes in memory, the last one dense. ``table``: int32 (n_requests, max_pages), the
     pages of each request in token order. ``lens``: int32 (n_requests), cached
     tokens. ``k_scale``, ``v_scale``: float32 (n_kv), 8-bit caches only.
 
@@ -683,7 +683,8 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
     """Attention of the newest tokens of a batch over its cache (ds_decode_attention).
 
     ``q``: (n_rows, n_tokens, n_q, head_dim), the queries of each request's
-    last n_tokens cached tokens, float16 or bfloat16; the last axis dense.
+    last n_tokens cached tokens, float16 or bfloat16; the last axis dense,
+    the other strides multiples of 8.
     ``rows``: int32 (n_rows), the request of each row, e.g. the head of an
     ``order`` permutation; None: row i is request i. ``scale``: 1 /
     sqrt(head_dim) by default. ``window``, ``sinks``: tokens seen back (0: all)
@@ -710,6 +711,8 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
         p_out = _arg(out, dev, q.dtype, shape, "out")
     p_mass = None if mass is None else _arg(mass, dev, torch.float32, _mass_shape(mass, cache), "mass")
     s_row, s_token, s_head, _ = q.stride()
+    if (s_row | s_token | s_head) & 7:                    # an axis of one entry may have any stride
+        s_row, s_token, s_head = [s if m > 1 else 0 for s, m in zip((s_row, s_token, s_head), shape)]
     p = ctypes.byref(DecodeParams(h, t, DTYPES[q.dtype], s_row, s_token, s_head, d ** -0.5 if scale is None else float(scale),
                                   int(window), int(sinks), int(max_len), 0 if mass is None else mass.shape[2]))
     p_ws, ws_bytes, ws = _scratch(ws, lib.ds_decode_workspace_bytes(cache.ref, p, n, mass is not None), q, dev, validate)

@@ -83,3 +83,19 @@ def test_values_near_the_end_of_bf16(ds, n, t, group, dim, page):
     assert torch.isfinite(out[:2]).all() and torch.isfinite(out[2, ..., :dim - 1]).all()
     ref.check_out(out.cpu(), want, off, BF16)
     ref.check_mass(dm.cpu(), m, m_off)
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 4), (3, 1, 4), (1, 2, 4), (2, 3, 1), (1, 1, 1)])
+def test_strides_of_single_entries(ds, shape):
+    """What torch holds as the stride of an axis of one entry has no meaning."""
+    n, t, h = shape
+    s = Setup(ds, [40] * n, 16, 1, 64, BF16, seed=3)
+    q = torch.randn((n, t, h, 64), generator=s.g).to(BF16)
+    want = ds.decode_attention(q.cuda(), s.cache)
+    strides = [7 if m == 1 else st for m, st in zip(shape, q.stride())] + [1]
+    odd = q.cuda().as_strided(q.shape, strides)
+    assert odd.is_contiguous() and torch.equal(ds.decode_attention(odd, s.cache, validate=True), want)
+    with pytest.raises(ds.DriftSchedError) as e:          # rows that begin between two 16-byte units
+        ds.decode_attention(torch.zeros((n + 1, t, h * 64 + 4), dtype=BF16, device="cuda")[:, :, :h * 64].unflatten(2, (h, 64)),
+                            Setup(ds, [40] * (n + 1), 16, 1, 64, BF16, seed=4).cache)
+    assert e.value.status == -7
