@@ -222,7 +222,7 @@ struct Attender {
 
     const DecodeArgs &a;
     Span span;
-    uint32_t row, head, tile, query_rows, n;
+    uint32_t n;
     int m, g, first_pos, lo;
     float scale;
     float down;                                                // what kCareful multiplies values with
@@ -628,11 +628,7 @@ void attend_kernel(const DecodeArgs a)
 
     A w{a};
     w.span = span;
-    w.row = row;
     w.req = req;
-    w.head = head;
-    w.tile = tile;
-    w.query_rows = query_rows;
     w.n = n;
     w.m = m;
     w.g = g;
