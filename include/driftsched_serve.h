@@ -53,7 +53,8 @@ typedef enum {
  * head h starts at element
  *     page * page_stride + slot * token_stride + h * head_stride
  * of k (its value: of v) and is head_dim elements long. Pages may be shared
- * between requests; any order of the axes page, slot and head fits.
+ * between requests (each request reads them for itself); any order of the axes
+ * page, slot and head fits.
  *
  *  k, v       device, 16-byte aligned; strides in elements, multiples of 16 bytes
  *  k_scale,   device, n_kv float, or NULL for ones; DS_E4M3 only (else NULL):
@@ -83,14 +84,14 @@ typedef struct {
 /* Parameters of ds_decode_attention. */
 typedef struct {
     uint32_t n_q;           /* query heads, a multiple of n_kv; head h reads head h / (n_q / n_kv) */
-    uint32_t n_tokens;      /* new tokens per row, 1..DS_MAX_NEW_TOKENS */
+    uint32_t n_tokens;      /* new tokens per row, 1..DS_MAX_NEW_TOKENS, the same for every row of a call */
     ds_dtype q_type;        /* of q and out: DS_F16 or DS_BF16; the cache's own type unless that is DS_E4M3 */
     uint64_t q_row_stride, q_token_stride, q_head_stride;   /* elements, multiples of 8 */
     double scale;           /* of the products q.k; finite */
     uint32_t window;        /* tokens a query sees back, itself included; 0: all */
     uint32_t sinks;         /* first tokens that stay visible behind the window */
     uint32_t max_len;       /* contract: len <= max_len for the batch's requests; 0: max_pages * page_size.
-                               Sizes the launch and the workspace */
+                               Sizes the launch and the workspace, whatever the requests hold */
     uint64_t mass_len;      /* entries of mass per request and head, >= max_len; unused without mass */
 } ds_decode_params;
 
@@ -108,7 +109,13 @@ typedef struct {
  * token j of request r and head h, the sum of w_j over the row's queries of
  * head h's group is stored in mass[(r * n_kv + h) * mass_len + j] for the
  * n_tokens newest tokens, and added to what stands there for the others.
- * Nothing is written from entry n on.
+ * Nothing is written from entry n on. Rows with different numbers of new
+ * tokens (drafts, say) therefore go in one call per number, each with its part
+ * of the batch as `rows`: given more queries than it has new tokens, a row
+ * would lose what its older tokens had gathered and count their queries again.
+ *
+ * Up to 1,024 rows a call splits long requests over the chip by the lengths of
+ * the whole batch; with more, one workgroup per head takes all of a request.
  *
  * Scores, softmax and sums are held in 32 bits; the weights enter the second
  * product as two parts of q's type, which hold a weight to 2^-17 (bfloat16) or
@@ -136,7 +143,8 @@ typedef struct {
     uint32_t sinks;         /* first tokens that always stay */
     uint32_t recent;        /* last tokens that always stay */
     uint32_t slack;         /* tokens a request may hold above its budget before it is cut */
-    uint32_t max_len;       /* as in ds_decode_params */
+    uint32_t max_len;       /* as in ds_decode_params; above 24,576 the workspace takes, per row and head,
+                               8 KB for each 8,192 tokens (at most 2 MB) and 4 bytes for each that may be kept */
     uint64_t mass_len;      /* entries of mass and mass_out per request and head, >= max_len */
     uint64_t kept_len;      /* entries of kept per row and head */
 } ds_evict_params;

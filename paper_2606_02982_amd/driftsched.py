@@ -689,10 +689,12 @@ def decode_attention(q, cache, rows=None, scale=None, window=0, sinks=0, max_len
     ``order`` permutation; None: row i is request i. ``scale``: 1 /
     sqrt(head_dim) by default. ``window``, ``sinks``: tokens seen back (0: all)
     and first tokens always seen. ``max_len``: the most tokens any request of
-    the batch holds, if known (a tighter launch and workspace). ``mass``:
-    float32 (n_requests, n_kv, length >= max_len), updated in place with the
-    weight each cached token received. ``out`` must not overlap q. Returns out,
-    shaped like q."""
+    the batch holds, if known (the launch and the workspace are sized by it, or
+    else by the table's width). ``mass``: float32 (n_requests, n_kv, length >=
+    max_len), updated in place with the weight each cached token received: set
+    for the n_tokens newest, added for the others. Rows with different numbers
+    of new tokens go in one call per number. ``out`` must not overlap q. Returns
+    out, shaped like q."""
     if type(window) is not int or type(sinks) is not int or type(max_len) is not int or (window | sinks | max_len) >> 32:
         _refuse_counts(window=window, sinks=sinks, max_len=max_len)
     if q.dim() != 4 or q.shape[3] != cache.head_dim or q.stride(3) != 1:
@@ -731,7 +733,8 @@ def cache_evict(cache, dst, budget, mass, rows=None, sinks=4, recent=64, slack=0
     the row was cut and copied; dst.lens may not be (part of) cache.lens. ``budget``: float64 (n_requests), e.g. from
     ``score``. ``mass``: as ``decode_attention`` leaves it. ``mass_out``: None
     updates mass in place. ``kept``: int32 (n_rows, n_kv, length); by default
-    as long as dst's rows. Returns (dst.lens, kept)."""
+    as long as dst's rows. ``max_len``: as in ``decode_attention``; without it a
+    wide table takes a large workspace. Returns (dst.lens, kept)."""
     if any(type(x) is not int or x >> 32 for x in (sinks, recent, slack, max_len)):
         _refuse_counts(sinks=sinks, recent=recent, slack=slack, max_len=max_len)
     dev = _device_of(budget)
