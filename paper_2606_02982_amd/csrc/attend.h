@@ -98,7 +98,13 @@ __device__ __forceinline__ float finite_or_zero(float m) { return m == -__builti
 
 typedef const __attribute__((address_space(4))) uint32_t *ScalarU32;   // read-only during the launch: scalar loads
 
-constexpr uint32_t kBalancedRows = 1024;   // rows whose lengths every workgroup looks through
+// Rows whose lengths every workgroup looks through. Above it every row is one
+// slot: looking through more rows costs more than the split gives where
+// lengths are alike, and a row far longer than the others then takes the time
+// of one workgroup per head (2 heads of 128 dimensions in 16 bits, up to 400
+// tokens, 1,025 rows split / not: 75 / 45 us, 2,048 rows 152 / 79 us; one
+// head, one row of 32,768 tokens among 1,025 of 64: 34 / 430 us).
+constexpr uint32_t kBalancedRows = 1024;
 
 __device__ __forceinline__ uint32_t length_of(const DecodeArgs &a, uint32_t row, uint32_t &req)
 {
@@ -192,10 +198,11 @@ __device__ inline Slots find_slots(const DecodeArgs &a, uint32_t want)
 // us, in pages of 24 tokens 128.)
 enum { kAnyPage, kPages16, kWhole };
 
-// A step takes as many blocks as make 16 KB of keys and values (8 KB for 64
-// dimensions in 8 bits), the same registers whatever the type: the chain of a
-// step (products, maximum over the lanes, exponentials, products) is as long
-// for few bytes as for many.
+// A step takes two blocks where one is 8 KB of keys and values or less and
+// there is one tile of query rows, else one (32 KB for 256 dimensions in 16
+// bits): the chain of a step (products, maximum over the lanes, exponentials,
+// products) is as long for few bytes as for many, and a second tile needs the
+// registers of the second block.
 template <int kDim, int kElem, int kTiles>
 constexpr int kSubBlocks = kDim * kElem >= 256 || kTiles > 1 ? 1 : 2;
 
@@ -291,13 +298,18 @@ struct Attender {
                (uint32_t)__shfl((int)(uint32_t)p.at, token, 64);
     }
 
-    // kStream: whole cache lines that no other workgroup reads go past the
-    // caches (16 heads of 128 dimensions in 16 bits: 380 -> 370 us for 2.1 GB,
-    // 8 heads of 256: 348 -> 336 us, 20 query rows 216 -> 199 us; in 8 bits
-    // 217 -> 222 us, 40 query rows, whose two units read the same, 268 -> 365
-    // us). Not where dimensions are missing: heads share lines, and the first
-    // dimensions are read again in place of the last (8 heads of 80: 116 us,
-    // streamed 160; of 192: 228 and 276).
+    // kStream: whole cache lines that no other unit of the pair reads go past
+    // the caches (16 heads of 128 dimensions in 16 bits: 380 -> 370 us for 2.1
+    // GB, 8 heads of 256: 348 -> 336 us, 20 query rows 216 -> 199 us; in 8
+    // bits 217 -> 222 us, 40 query rows, whose two units read the same, 268 ->
+    // 365 us). Not where dimensions are missing: heads share lines, and the
+    // first dimensions are read again in place of the last (8 heads of 80: 116
+    // us, streamed 160; of 192: 228 and 276).
+    // Which requests share pages the host does not know, and such pages would
+    // gain from the caches (32 requests of 8,192 tokens, 8 heads of 128
+    // dimensions in 16 bits, streamed / not: none shared 176 / 193 us, the
+    // first half 161 / 123, all 145 / 83; 8 heads of 256, 16 requests: 175 /
+    // 185, 141 / 132 and 116 / 102).
     template <typename W>
     static __device__ __forceinline__ W fetch(const uint8_t *p)
     {
@@ -571,9 +583,11 @@ struct Attender {
 };
 
 // Waves per SIMD that the registers are limited to: as many as fit without
-// spills. kFast: kWhole, and kPages16 with two tiles of query rows (24 rows, 8
-// heads of 80 dimensions, 671 MB: 161 us, with one wave less 171; for one tile
-// 125 us for 481 MB, with one wave less 116).
+// spilling vector registers (scalar ones are spilled into lanes of these in
+// most of the kernels, up to 33). kFast: kWhole, and kPages16 with two tiles of
+// query rows (24 rows, 8 heads of 80 dimensions, 671 MB: 161 us, with one wave
+// less 171; of 48, 302 MB: 98 and 99 us, in 8 bits 72 and 71; for one tile of
+// 80 125 us for 481 MB, with one wave less 116).
 template <int kWidth, int kSub, bool kFast>
 constexpr int kWaves = kWidth <= 64 ? (kSub == 1 || kFast ? 3 : 2) : kWidth <= 128 ? (kSub == 1 && kFast ? 3 : 2) : kWidth <= 256 && kFast ? 2 : 1;
 
@@ -598,7 +612,10 @@ void attend_kernel(const DecodeArgs a)
     //    bytes, a cache line (8-bit, 8 heads: 64 dimensions 92 -> 69 us for
     //    268 MB, 128 dimensions 119 -> 116 us for 537 MB), or ends inside a
     //    line (8 heads of 80 dimensions in 16 bits 128 -> 116 us for 481 MB,
-    //    of 96 130 -> 118 us for 577 MB);
+    //    of 96 130 -> 118 us for 577 MB), and there are 64 slots, eight for
+    //    each die (80 dimensions in 16 bits, requests of 2,048 tokens, a die
+    //    per slot / slots first: 128 slots 26 / 31 us, 64 slots 17 / 20, 32
+    //    slots 15 / 17, 8 slots 14 / 15; with one slot one die has it all);
     //  - all slots of few heads, up to 8 heads (8 heads of 128 dimensions in
     //    16 bits: 192 -> 177 us for 1.07 GB, three long rows 241 -> 222 us
     //    for 1.33 GB); the odd number of slots spreads a slot's heads over

@@ -35,7 +35,7 @@ void decode_plan(DecodeArgs &a)
     // only two workgroups fit a compute unit (16 rows of 1,024 visible tokens
     // and 40 query rows: 640 workgroups in two rounds 27 us, 384 in one 19 us)
     a.slot_blocks = unit_rows > 16 ? 16 : 8;
-    // no row can be cut, or so many rows that none need be: one slot each
+    // no row can be cut, or more rows than each workgroup looks through: one slot each
     a.slot_goal = blocks > a.slot_blocks && a.n_rows <= kBalancedRows ? (uint32_t)cdiv(unit_goal(key_bytes, unit_rows / 16), a.c.n_kv * a.n_tiles) : 0;
     a.n_slots = a.n_rows;
     if (a.slot_goal) {
@@ -43,7 +43,7 @@ void decode_plan(DecodeArgs &a)
         const uint64_t most = (uint64_t)a.n_rows * cdiv(blocks, a.slot_blocks);
         a.n_slots = (uint32_t)(a.slot_goal + a.n_rows < most ? a.slot_goal + a.n_rows : most);
     }
-    // a die per slot needs slots for every die
+    // a die per slot where every die gets several (attend_kernel)
     a.spread = (key_bytes <= 128 || key_bytes % 128) && a.n_slots >= 64 ? kDieOfSlot : a.c.n_kv <= 8 ? kSlotsFirst : kHeadsFirst;
 }
 

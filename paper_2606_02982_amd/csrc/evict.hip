@@ -553,7 +553,10 @@ __device__ __forceinline__ void put(uint8_t *to, const uint8_t *from)
 // caches, and the heads of one piece to one die (dies take workgroups in turn)
 // (32 rows of 2,000 to 6,000 tokens, 8 heads, kShared / not: 80 dimensions in
 // 16 bits 97 / 148 us, in 8 bits 76 / 118, 64 in 8 bits 56 / 64; 128 in 16
-// bits 121 / 116).
+// bits 121 / 116). Taken from 64 pieces of all rows on, eight for each die (80
+// dimensions in 16 bits, whole call, kShared / not: 16 rows of 2,000 tokens
+// 34.6 / 38.5 us, 3 rows, 72 pieces, 17.5 / 19.2; below, 2 rows, 48 pieces,
+// 16.6 / 17.9, one row, 24 pieces, 15.0 / 15.0).
 template <bool kShared>
 __global__ __launch_bounds__(256) void copy_kernel(const EvictArgs a, uint32_t groups, uint32_t tokens, uint32_t elem)
 {
