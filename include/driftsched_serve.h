@@ -19,7 +19,8 @@
  * point" holds here too: device arrays, host parameter structs, workspaces of
  * the caller, enqueueing on the caller's stream, status codes, DS_VALIDATE.
  * `rows` names the batch: rows[i] is the request of row i, e.g. the first
- * n_rows entries of a ds_order permutation; NULL: row i is request i. A
+ * n_rows entries of a ds_order permutation; NULL: row i is request i. What a
+ * call writes lies apart from what it reads, but where it says otherwise. A
  * workspace of 256 bytes is used by DS_VALIDATE only and may be NULL without
  * that flag.
  */
